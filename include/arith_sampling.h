@@ -430,6 +430,152 @@ as_status as_encode(as_ctx *ctx, const as_model *model, const int32_t *prompts,
                     int32_t top_k, float top_p, int32_t eos_id,
                     double *lo_out, double *width_out);
 
+/* ------------------------------------------------ layers and shaped logits */
+
+/*
+ * What a decode with a model of the caller's own needs around as_step: the
+ * layers in front of the logits (as_linear), the modifiers that serving puts
+ * on the logits before they are sampled from (as_shape_logits, or the last
+ * layer's as_linear with a shaping), and the record of each sequence's tokens
+ * that the penalties among them go by (as_history_set, as_history_add).
+ * All of them work on the context's stream; none looks at the context's
+ * vocabulary but as_shape_logits.
+ */
+typedef struct as_layer as_layer;
+
+typedef enum {
+    AS_ACT_NONE = 0,
+    AS_ACT_RELU = 1,      /* max(z, 0)                                               */
+    AS_ACT_GELU = 2,      /* z/2 * (1 + erf(z / sqrt 2))                             */
+    AS_ACT_GELU_TANH = 3, /* z/2 * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3)))       */
+    AS_ACT_SILU = 4,      /* z / (1 + exp(-z))                                       */
+    AS_ACT_SOFTCAP = 5    /* act_arg * tanh(z / act_arg), act_arg > 0: capped logits */
+} as_act;
+
+/*
+ * Modifiers of logits, applied to each logit y[r, v] in this order (fp32):
+ *   1. repetition   where token v is seen in row r: y / repetition[r] if y > 0,
+ *                   else y * repetition[r]
+ *   2. frequency, presence   y - frequency[r] * n - (n > 0 ? presence[r] : 0),
+ *                   n the count of token v in row r
+ *   3. bias         y + bias[bias_ids[r], v]
+ *   4. mask         -inf where the bit of token v in mask[mask_ids[r]] is 0
+ *                   (whatever y was, NaN among it)
+ * A member that is NULL is left out.  All pointers are DEVICE pointers.  A row
+ * whose mask leaves nothing becomes all -inf (as_step emits some token in
+ * range for it); a bias of -inf forbids a token as the mask does.
+ *   seen, seen_ld       uint32[rows, seen_ld]: token v is bit v % 32 of word
+ *                       v / 32; seen_ld >= ceil(V / 32); bits past V are ignored.
+ *                       Needed with any of the three strengths.
+ *   counts, counts_ld   int32[rows, counts_ld], counts_ld >= V; read only where
+ *                       the seen bit is set.  Needed with frequency or presence.
+ *   repetition          float[rows], each > 0
+ *   presence, frequency float[rows]
+ *   bias, bias_ld, bias_rows   float[bias_rows, bias_ld], bias_ld >= V
+ *   bias_ids            int32[rows]: the row of `bias` that a row takes, < 0: none
+ *                       (past the end: the last); NULL: row r, or the only one
+ *   mask, mask_ld, mask_rows, mask_ids   the same for uint32[mask_rows, mask_ld],
+ *                       bits as in seen
+ *   finished            uint8[rows]: rows with a non-zero flag are left out: their
+ *                       logits are neither read nor written
+ */
+typedef struct as_shaping {
+    const uint32_t *seen;
+    int64_t seen_ld;
+    const int32_t *counts;
+    int64_t counts_ld;
+    const float *repetition, *presence, *frequency;
+    const float *bias;
+    int64_t bias_ld, bias_rows;
+    const int32_t *bias_ids;
+    const uint32_t *mask;
+    int64_t mask_ld, mask_rows;
+    const int32_t *mask_ids;
+    const uint8_t *finished;
+} as_shaping;
+
+/*
+ * logits_out[r, :V] = logits[r, :V] shaped, rounded once to the context's
+ * logits dtype.  logits_out may be logits (same ld_out); otherwise the two must
+ * not overlap.  Rows may start anywhere and be any stride >= V apart; columns
+ * V.. of a row are neither read nor written.
+ */
+as_status as_shape_logits(as_ctx *ctx, const void *logits, int64_t rows, int64_t ld,
+                          const as_shaping *shaping, void *logits_out, int64_t ld_out);
+
+/*
+ * A layer y = act(scale * x W^T + bias).
+ *   W        DEVICE [n, k] row-major, wdtype, rows ldw >= k apart
+ *   bias     DEVICE [n], wdtype, or NULL; read once here
+ *   act_arg  of AS_ACT_SOFTCAP, otherwise ignored
+ * W is borrowed, must outlive the layer and keep its contents where it is fp32
+ * or its rows start on 16 bytes and k is a multiple of 64; other bf16 weights
+ * are read once here (the layer keeps a copy in rows of that kind).  The call
+ * enqueues kernels on the default stream and waits for them.
+ */
+as_status as_layer_create(as_layer **out, const void *W, int64_t ldw, const void *bias,
+                          int32_t n, int32_t k, float scale, as_act act, float act_arg,
+                          as_dtype wdtype);
+as_status as_layer_destroy(as_layer *layer);
+
+/*
+ * out[r, :n] = act(scale * x[r, :k] W^T + bias) + residual[r, :n], shaped if
+ * `shaping` is given (with V = n), for r < rows: sums and all that follows in
+ * fp32, rounded once to out_dtype.  A bf16 layer's products run on the bf16
+ * matrix instructions, an fp32 layer's on the fp32 ones.
+ *   x          DEVICE [rows, k], the layer's wdtype, rows ldx >= k apart
+ *   residual   DEVICE [rows, n], out_dtype, rows ldr >= n apart, or NULL; may be
+ *              `out` itself (ldr = ldo)
+ *   shaping    or NULL
+ *   out        DEVICE [rows, n], out_dtype, rows ldo >= n apart; must not overlap x
+ *   out_dtype  AS_F32, or AS_BF16 from a bf16 layer
+ * Rows may start anywhere; columns n.. of out are not written.  rows may be 0 and
+ * at most the context's max_rows.  bf16 rows of x that do not start on 16 bytes,
+ * or a k that is no multiple of 64, take room for a copy of x in the context,
+ * (re)allocated when a call needs more than any earlier one did, and narrow
+ * products 32 MiB once: such a first call must not be made under stream capture.
+ */
+as_status as_linear(as_ctx *ctx, const as_layer *layer, const void *x, int64_t rows,
+                    int64_t ldx, const void *residual, int64_t ldr,
+                    const as_shaping *shaping, void *out, int64_t ldo,
+                    as_dtype out_dtype);
+
+/*
+ * The record that repetition, frequency and presence go by, of `rows` sequences:
+ * which tokens each has seen, and how often it has emitted each, in buffers of
+ * the caller's (seen and counts as in as_shaping) that start out as zeros and are
+ * then changed by these two calls alone.  V is the context's.
+ *
+ * as_history_set: row r's record becomes that of its prompt and its own tokens.
+ * Tokens of the prompt are seen, the row's own are seen and counted.
+ *   counts          may be NULL: nothing is counted
+ *   which           DEVICE uint8[rows] or NULL: rows with a zero flag are left alone
+ *   prompts, prompt_offsets, prompts_len, rows_per_prompt
+ *                   prompts DEVICE int32[prompts_len], all prompts one after the
+ *                   other; row r has prompts[prompt_offsets[p] .. prompt_offsets[p+1])
+ *                   with p = r / rows_per_prompt; prompt_offsets DEVICE int64 (one
+ *                   more than there are prompts); prompts may be NULL: none
+ *   tokens, tokens_ld, T, lens
+ *                   DEVICE int32[rows, tokens_ld]: row r has emitted its first
+ *                   lens[r] (at most T) tokens, all T where lens (DEVICE int32[rows])
+ *                   is NULL; tokens may be NULL: none
+ *
+ * as_history_add: one token more for each row, counted: what a step emitted.
+ *   tokens          DEVICE int32[rows]
+ *   finished        DEVICE uint8[rows] or NULL: rows with a non-zero flag add nothing
+ *
+ * Tokens outside [0, V) are left out.  Both calls allocate nothing.
+ */
+as_status as_history_set(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *counts,
+                         int64_t counts_ld, int64_t rows, const uint8_t *which,
+                         const int32_t *prompts, const int64_t *prompt_offsets,
+                         int64_t prompts_len, int32_t rows_per_prompt,
+                         const int32_t *tokens, int64_t tokens_ld, int32_t T,
+                         const int32_t *lens);
+as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *counts,
+                         int64_t counts_ld, int64_t rows, const int32_t *tokens,
+                         const uint8_t *finished);
+
 #ifdef __cplusplus
 }
 #endif

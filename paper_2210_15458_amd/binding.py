@@ -17,6 +17,18 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libarith_sa
 _lib = None
 
 
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4, "softcap": 5}
+
+
+class _Shaping(C.Structure):
+    """as_shaping."""
+    _fields_ = [("seen", C.c_void_p), ("seen_ld", C.c_int64), ("counts", C.c_void_p), ("counts_ld", C.c_int64),
+                ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("bias", C.c_void_p), ("bias_ld", C.c_int64), ("bias_rows", C.c_int64), ("bias_ids", C.c_void_p),
+                ("mask", C.c_void_p), ("mask_ld", C.c_int64), ("mask_rows", C.c_int64), ("mask_ids", C.c_void_p),
+                ("finished", C.c_void_p)]
+
+
 class ArithSamplingError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{_STATUS.get(code, code)}: {msg}")
@@ -53,6 +65,13 @@ def lib():
     L.as_decode_fused.argtypes = [vp, vp, vp, i32, i32, i32, vp, f32, i32, vp, vp]
     L.as_bigram_group_mass.argtypes = [vp, vp, vp, i64, f32, vp, i64]
     L.as_step_fused.argtypes = [vp, vp, vp, i64, vp, i64, vp, f32, vp, vp, vp, i32, vp]
+    shaping = C.POINTER(_Shaping)
+    L.as_shape_logits.argtypes = [vp, vp, i64, i64, shaping, vp, i64]
+    L.as_layer_create.argtypes = [C.POINTER(vp), vp, i64, vp, i32, i32, f32, C.c_int, f32, C.c_int]
+    L.as_layer_destroy.argtypes = [vp]
+    L.as_linear.argtypes = [vp, vp, vp, i64, i64, vp, i64, shaping, vp, i64, C.c_int]
+    L.as_history_set.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, vp, i64, i32, vp, i64, i32, vp]
+    L.as_history_add.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp]
     L.as_ctx_set_tuning.argtypes = [vp, C.c_int, i32]
     L.as_ctx_set_tuning.restype = C.c_int
     L.as_ctx_profile.argtypes = [vp, C.c_int]
@@ -64,7 +83,8 @@ def lib():
     for name in ("as_ctx_create", "as_ctx_destroy", "as_step", "as_step_ex", "as_step_static", "as_lattice",
                  "as_model_create_bigram", "as_model_destroy", "as_bigram_logits", "as_decode",
                  "as_interval_step", "as_encode", "as_decode_ancestral", "as_estimate_mean", "as_decode_fused",
-                 "as_bigram_group_mass", "as_step_fused"):
+                 "as_bigram_group_mass", "as_step_fused", "as_shape_logits", "as_layer_create", "as_layer_destroy",
+                 "as_linear", "as_history_set", "as_history_add"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -302,3 +322,131 @@ def as_step_fused(ctx, model, mass, prev, codes, temp, tokens_out, codes_out, fi
         _dev(codes, torch.float32, "codes", rows), float(temp), _dev(tokens_out, torch.int32, "tokens_out", rows),
         _dev(codes_out, torch.float32, "codes_out", rows), _dev(finished_in, torch.uint8, "finished_in", rows),
         int(eos_id), _dev(finished_out, torch.uint8, "finished_out", rows)))
+
+
+# ------------------------------------------------------------------------------------------ layers and shaped logits
+
+def _rows(t, dtype, name, rows, cols):
+    """Pointer and row stride of a 2-D GPU tensor whose rows are contiguous, of `rows` rows and at least `cols` columns."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    (r, c), (ld, one) = t.shape, t.stride()
+    if r < rows or c < cols:
+        raise ValueError(f"{name} is {r} x {c}, needs {rows} x {cols}")
+    if one != 1 and c > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if r < 2:
+        ld = c                            # (one row: its stride says nothing)
+    elif ld < c:
+        raise ValueError(f"{name} has rows that overlap")
+    return t.data_ptr(), ld
+
+
+class Layer:
+    """as_layer: act(scale * x W^T + bias) for W [n, k] (borrows W where the library does not lay it out anew)."""
+
+    def __init__(self, W, bias=None, act="none", act_arg=0.0, scale=1.0):
+        if not isinstance(W, torch.Tensor) or W.dim() != 2:
+            raise ValueError("W must be [n, k]")
+        if act not in ACTS:
+            raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTS)}")
+        self.n, self.k = W.shape
+        self.torch_dtype = W.dtype
+        self._W = W                       # keep the borrowed tensor alive
+        self._h = C.c_void_p()
+        ptr, ld = _rows(W, W.dtype, "W", self.n, self.k)
+        rc = lib().as_layer_create(C.byref(self._h), ptr, ld, _dev(bias, W.dtype, "bias", self.n), self.n, self.k, float(scale),
+                                   ACTS[act], float(act_arg), _dtype_code(W))
+        if rc != 0:
+            raise ArithSamplingError(rc, (lib().as_last_error(None) or b"").decode())
+
+    def close(self):
+        if self._h:
+            lib().as_layer_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Shaping:
+    """as_shaping for `rows` rows of V logits: checked once, and the tensors kept alive; their contents may change from
+    call to call.  Bit words (seen, mask) are int32 tensors."""
+
+    def __init__(self, rows, V, seen=None, counts=None, repetition=None, presence=None, frequency=None, bias=None,
+                 bias_ids=None, mask=None, mask_ids=None, finished=None):
+        self.rows, self.V = int(rows), int(V)
+        words = (self.V + 31) // 32
+        self._tensors = (seen, counts, repetition, presence, frequency, bias, bias_ids, mask, mask_ids, finished)
+        c = self._c = _Shaping()
+        if seen is not None:
+            c.seen, c.seen_ld = _rows(seen, torch.int32, "seen", self.rows, words)
+        if counts is not None:
+            c.counts, c.counts_ld = _rows(counts, torch.int32, "counts", self.rows, self.V)
+        if bias is not None:
+            c.bias, c.bias_ld = _rows(bias, torch.float32, "bias", 1, self.V)
+            c.bias_rows = bias.shape[0]
+        if mask is not None:
+            c.mask, c.mask_ld = _rows(mask, torch.int32, "mask", 1, words)
+            c.mask_rows = mask.shape[0]
+        for name, t, dtype in (("repetition", repetition, torch.float32), ("presence", presence, torch.float32),
+                               ("frequency", frequency, torch.float32), ("bias_ids", bias_ids, torch.int32),
+                               ("mask_ids", mask_ids, torch.int32), ("finished", finished, torch.uint8)):
+            if t is not None:
+                setattr(c, name, _dev(t, dtype, name, self.rows))
+        self._ref = C.byref(c)
+
+
+def _shaping_ref(shaping, rows, V):
+    if shaping.rows < rows or shaping.V != V:
+        raise ValueError(f"shaping is for {shaping.rows} x {shaping.V} logits, not {rows} x {V}")
+    return shaping._ref
+
+
+def as_shape_logits(ctx, logits, shaping, logits_out):
+    """The first V columns of logits [rows, >= V], shaped, to logits_out (which may be logits)."""
+    rows = logits.shape[0]
+    ptr, ld = _rows(logits, ctx.torch_dtype, "logits", rows, ctx.V)
+    out, ldo = _rows(logits_out, ctx.torch_dtype, "logits_out", rows, ctx.V)
+    ctx._check(lib().as_shape_logits(ctx._h, ptr, rows, ld, _shaping_ref(shaping, rows, ctx.V), out, ldo))
+
+
+def as_linear(ctx, layer, x, out, residual=None, shaping=None):
+    rows = x.shape[0]
+    xp, ldx = _rows(x, layer.torch_dtype, "x", rows, layer.k)
+    op, ldo = _rows(out, out.dtype, "out", rows, layer.n)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, out.dtype, "residual", rows, layer.n)
+    ctx._check(lib().as_linear(ctx._h, layer._h, xp, rows, ldx, rp, ldr,
+                               None if shaping is None else _shaping_ref(shaping, rows, layer.n), op, ldo, _dtype_code(out)))
+
+
+def as_history_set(ctx, seen, counts, prompts=None, prompt_offsets=None, rows_per_prompt=1, tokens=None, lens=None, which=None):
+    """The record (seen [rows, words], counts [rows, >= V] or None) of ragged prompts and of tokens [rows, T]."""
+    rows = seen.shape[0]
+    sp, sld = _rows(seen, torch.int32, "seen", rows, (ctx.V + 31) // 32)
+    cp, cld = (None, 0) if counts is None else _rows(counts, torch.int32, "counts", rows, ctx.V)
+    pp, po, plen = None, None, 0
+    if prompts is not None:
+        plen, pp = prompts.numel(), _dev(prompts, torch.int32, "prompts")
+        po = _dev(prompt_offsets, torch.int64, "prompt_offsets", (rows - 1) // int(rows_per_prompt) + 2)
+    tp, tld, T = None, 0, 0
+    if tokens is not None:
+        tp, tld = _rows(tokens, torch.int32, "tokens", rows, 0)
+        T = tokens.shape[1]
+    ctx._check(lib().as_history_set(ctx._h, sp, sld, cp, cld, rows, _dev(which, torch.uint8, "which", rows), pp, po, plen,
+                                    int(rows_per_prompt), tp, tld, T, _dev(lens, torch.int32, "lens", rows)))
+
+
+def as_history_add(ctx, seen, counts, tokens, finished=None):
+    rows = seen.shape[0]
+    sp, sld = _rows(seen, torch.int32, "seen", rows, (ctx.V + 31) // 32)
+    cp, cld = (None, 0) if counts is None else _rows(counts, torch.int32, "counts", rows, ctx.V)
+    ctx._check(lib().as_history_add(ctx._h, sp, sld, cp, cld, rows, _dev(tokens, torch.int32, "tokens", rows),
+                                    _dev(finished, torch.uint8, "finished", rows)))

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libarith_sampling.so")
 SOURCES = ["as_api.hip", "as_step.hip", "as_threshold.hip", "as_wide.hip", "as_model.hip", "as_interval.hip", "as_fused.hip",
-           "as_small.hip", "as_rows.hip"]
+           "as_small.hip", "as_rows.hip", "as_linear.hip", "as_shape.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -31,6 +31,7 @@ def stale():
         return True
     t = os.path.getmtime(OUT)
     deps = sources() + [os.path.join(CSRC, "as_common.hpp"), os.path.join(CSRC, "as_row.hpp"), os.path.join(CSRC, "as_tile.hpp"), os.path.join(CSRC, "as_pairs.hpp"),
+                        os.path.join(CSRC, "as_shape.hpp"),
                         os.path.join(CSRC, "as_workspace.hpp"),
                         os.path.join(HERE, "..", "include", "arith_sampling.h")]
     return any(os.path.getmtime(d) > t for d in deps)

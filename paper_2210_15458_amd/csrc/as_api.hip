@@ -1,6 +1,6 @@
 // extern "C" entry points: argument checks on the host, then kernel launches on
 // the context's stream.  No entry point synchronises the device except
-// as_ctx_destroy and as_model_create_bigram / as_model_destroy.
+// as_ctx_destroy, as_model_create_bigram / as_model_destroy and as_layer_create / as_layer_destroy.
 #include <math.h>
 #include <stdlib.h>
 
@@ -177,6 +177,45 @@ static as_status check_step(as_ctx *ctx, const void *logits, int64_t rows, int64
     return AS_OK;
 }
 
+// The record's shape, as the shaping that reads it and the calls that write it have it.
+static as_status check_record(as_ctx *ctx, const void *seen, int64_t seen_ld, const void *counts, int64_t counts_ld, int32_t V)
+{
+    if (seen_ld < (V + 31) / 32) return fail(ctx, AS_ERR_INVALID_ARG, "seen_ld is smaller than ceil(V / 32)");
+    if (counts && counts_ld < V) return fail(ctx, AS_ERR_INVALID_ARG, "counts_ld is smaller than V");
+    if (reinterpret_cast<uintptr_t>(seen) % 4 != 0 || reinterpret_cast<uintptr_t>(counts) % 4 != 0)
+        return fail(ctx, AS_ERR_INVALID_ARG, "seen or counts is not aligned to its element type");
+    return AS_OK;
+}
+
+// A shaping of `rows` rows of V logits: checked, and `s` without the members that nothing in it uses.
+static as_status check_shaping(as_ctx *ctx, const as_shaping *given, int64_t rows, int32_t V, as_shaping *s)
+{
+    *s = *given;
+    if (!s->repetition && !s->presence && !s->frequency) s->seen = nullptr;
+    else if (!s->seen) return fail(ctx, AS_ERR_INVALID_ARG, "repetition, presence and frequency need seen");
+    if (!s->presence && !s->frequency) s->counts = nullptr;
+    else if (!s->counts) return fail(ctx, AS_ERR_INVALID_ARG, "presence and frequency need counts");
+    if (s->seen) {
+        const as_status st = check_record(ctx, s->seen, s->seen_ld, s->counts, s->counts_ld, V);
+        if (st != AS_OK) return st;
+    }
+    if (s->bias) {
+        if (s->bias_ld < V) return fail(ctx, AS_ERR_INVALID_ARG, "bias_ld is smaller than V");
+        if (s->bias_rows < 1 || (!s->bias_ids && s->bias_rows != 1 && s->bias_rows < rows))
+            return fail(ctx, AS_ERR_INVALID_ARG, "bias_rows must be 1, or a row for each where bias_ids is NULL");
+        if (reinterpret_cast<uintptr_t>(s->bias) % 4 != 0) return fail(ctx, AS_ERR_INVALID_ARG, "bias is not aligned to its element type");
+    }
+    if (s->mask) {
+        if (s->mask_ld < (V + 31) / 32) return fail(ctx, AS_ERR_INVALID_ARG, "mask_ld is smaller than ceil(V / 32)");
+        if (s->mask_rows < 1 || (!s->mask_ids && s->mask_rows != 1 && s->mask_rows < rows))
+            return fail(ctx, AS_ERR_INVALID_ARG, "mask_rows must be 1, or a row for each where mask_ids is NULL");
+        if (reinterpret_cast<uintptr_t>(s->mask) % 4 != 0) return fail(ctx, AS_ERR_INVALID_ARG, "mask is not aligned to its element type");
+    }
+    return AS_OK;
+}
+
+static bool aligned_to(const void *p, as_dtype t) { return reinterpret_cast<uintptr_t>(p) % (t == AS_BF16 ? 2 : 4) == 0; }
+
 }  // namespace as
 
 using namespace as;
@@ -229,6 +268,7 @@ as_status as_ctx_destroy(as_ctx *ctx)
     if (ctx->state.ptr) (void)hipFree(ctx->state.ptr);
     if (ctx->encode_logits.ptr) (void)hipFree(ctx->encode_logits.ptr);
     if (ctx->encode_state.ptr) (void)hipFree(ctx->encode_state.ptr);
+    if (ctx->linear_x.ptr) (void)hipFree(ctx->linear_x.ptr);
     for (auto &v : ctx->prof.slots)
         for (auto &s : v) {
             (void)hipEventDestroy(s.start);
@@ -1029,6 +1069,150 @@ as_status as_encode(as_ctx *ctx, const as_model *model, const int32_t *prompts, 
     if (isnan(top_p)) return fail(ctx, AS_ERR_INVALID_ARG, "top_p is NaN");
 
     return encode_windows(ctx, model, prompts, R, N, T, tokens, temp, top_k, top_p, eos_id, lo_out, width_out);
+}
+
+as_status as_shape_logits(as_ctx *ctx, const void *logits, int64_t rows, int64_t ld, const as_shaping *shaping,
+                          void *logits_out, int64_t ld_out)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    if (rows < 0 || rows > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "rows outside [0, max_rows]");
+    if (!shaping) return fail(ctx, AS_ERR_INVALID_ARG, "shaping is NULL");
+    if (rows == 0) return AS_OK;
+    if (!logits || !logits_out) return fail(ctx, AS_ERR_INVALID_ARG, "logits and logits_out must not be NULL");
+    if (ld < ctx->V || ld_out < ctx->V) return fail(ctx, AS_ERR_INVALID_ARG, "ld is smaller than the vocabulary");
+    if (logits == logits_out && ld != ld_out) return fail(ctx, AS_ERR_INVALID_ARG, "logits shaped in place with another ld_out");
+    if (!aligned_to(logits, ctx->dtype) || !aligned_to(logits_out, ctx->dtype))
+        return fail(ctx, AS_ERR_INVALID_ARG, "logits pointer is not aligned to its element type");
+    as_shaping s;
+    const as_status st = check_shaping(ctx, shaping, rows, ctx->V, &s);
+    if (st != AS_OK) return st;
+    return launch_shape(ctx, s, logits, rows, ld, logits_out, ld_out);
+}
+
+as_status as_layer_create(as_layer **out, const void *W, int64_t ldw, const void *bias, int32_t n, int32_t k, float scale,
+                          as_act act, float act_arg, as_dtype wdtype)
+{
+    if (!out) return fail(nullptr, AS_ERR_INVALID_ARG, "out is NULL");
+    *out = nullptr;
+    if (!W) return fail(nullptr, AS_ERR_INVALID_ARG, "W is NULL");
+    if (n < 1 || n > AS_MAX_VOCAB || k < 1 || k > AS_MAX_VOCAB)
+        return fail(nullptr, AS_ERR_INVALID_ARG, "n or k outside [1, AS_MAX_VOCAB]");
+    if (ldw < k) return fail(nullptr, AS_ERR_INVALID_ARG, "ldw is smaller than k");
+    if (wdtype != AS_F32 && wdtype != AS_BF16) return fail(nullptr, AS_ERR_INVALID_ARG, "unknown weight dtype");
+    if (act < AS_ACT_NONE || act > AS_ACT_SOFTCAP) return fail(nullptr, AS_ERR_INVALID_ARG, "unknown activation");
+    if (!isfinite(scale)) return fail(nullptr, AS_ERR_INVALID_ARG, "scale must be finite");
+    if (act == AS_ACT_SOFTCAP && (!(act_arg > 0.f) || !isfinite(act_arg) || !isfinite(1.f / act_arg)))
+        return fail(nullptr, AS_ERR_INVALID_ARG, "the cap must be finite and > 0");
+    if (!aligned_to(W, wdtype) || !aligned_to(bias, wdtype))
+        return fail(nullptr, AS_ERR_INVALID_ARG, "W or bias is not aligned to its element type");
+    as_layer *l = new (std::nothrow) as_layer();
+    if (!l) return fail(nullptr, AS_ERR_ALLOC, "host allocation failed");
+    l->n = n; l->k = k; l->wdtype = wdtype; l->act = act; l->act_arg = act_arg; l->scale = scale;
+    l->W = W; l->ldw = ldw; l->kp = k;
+    bool ok = hipMalloc(reinterpret_cast<void **>(&l->bias), (size_t)((n + 255) / 256 * 256) * sizeof(float)) == hipSuccess;
+    if (!ok) l->bias = nullptr;
+    if (wdtype == AS_BF16) {
+        l->kp = (k + 63) / 64 * 64;
+        if (l->kp != k || ldw % 8 != 0 || reinterpret_cast<uintptr_t>(W) % 16 != 0) {
+            ok = ok && hipMalloc(&l->own, (size_t)n * l->kp * 2) == hipSuccess;
+            if (!ok) l->own = nullptr;
+            l->W = l->own;
+            l->ldw = l->kp;
+        }
+    }
+    as_status st = AS_OK;
+    if (!ok) {
+        (void)hipGetLastError();
+        st = fail(nullptr, AS_ERR_ALLOC, "device allocation of the layer failed");
+    } else {
+        st = launch_layer_layout(*l, W, ldw, bias);
+    }
+    if (st != AS_OK) {
+        if (l->bias) (void)hipFree(l->bias);
+        if (l->own) (void)hipFree(l->own);
+        delete l;
+        return st;
+    }
+    *out = l;
+    return AS_OK;
+}
+
+as_status as_layer_destroy(as_layer *layer)
+{
+    if (!layer) return AS_OK;
+    (void)hipDeviceSynchronize();
+    if (layer->bias) (void)hipFree(layer->bias);
+    if (layer->own) (void)hipFree(layer->own);
+    delete layer;
+    return AS_OK;
+}
+
+as_status as_linear(as_ctx *ctx, const as_layer *layer, const void *x, int64_t rows, int64_t ldx, const void *residual,
+                    int64_t ldr, const as_shaping *shaping, void *out, int64_t ldo, as_dtype out_dtype)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    if (!layer) return fail(ctx, AS_ERR_INVALID_ARG, "layer is NULL");
+    if (rows < 0 || rows > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "rows outside [0, max_rows]");
+    if (out_dtype != AS_F32 && out_dtype != AS_BF16) return fail(ctx, AS_ERR_INVALID_ARG, "unknown output dtype");
+    if (layer->wdtype == AS_F32 && out_dtype != AS_F32) return fail(ctx, AS_ERR_UNSUPPORTED, "an fp32 layer has fp32 outputs");
+    if (rows == 0) return AS_OK;
+    if (!x || !out) return fail(ctx, AS_ERR_INVALID_ARG, "x and out must not be NULL");
+    if (ldx < layer->k || ldo < layer->n || (residual && ldr < layer->n))
+        return fail(ctx, AS_ERR_INVALID_ARG, "ldx, ldr or ldo is smaller than its rows");
+    if (!aligned_to(x, layer->wdtype) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype))
+        return fail(ctx, AS_ERR_INVALID_ARG, "x, residual or out is not aligned to its element type");
+    if (residual == out && ldr != ldo) return fail(ctx, AS_ERR_INVALID_ARG, "a residual added in place has the stride of out");
+    LinearArgs a{};
+    a.x = x; a.rows = rows; a.ldx = ldx; a.W = layer->W; a.ldw = layer->ldw; a.n = layer->n; a.k = layer->k;
+    a.bias = layer->bias; a.scale = layer->scale; a.act = layer->act; a.act_arg = layer->act_arg;
+    a.act_inv = layer->act == AS_ACT_SOFTCAP ? 1.f / layer->act_arg : 0.f;
+    a.residual = residual; a.ldr = ldr; a.out = out; a.ldo = ldo; a.out_dtype = out_dtype;
+    as_status st = AS_OK;
+    if (shaping) {
+        st = check_shaping(ctx, shaping, rows, layer->n, &a.shape);
+        if (st != AS_OK) return st;
+        a.shaped = true;
+    }
+    st = grow(ctx, ctx->linear_x, linear_workspace(layer, x, rows, ldx));
+    if (st != AS_OK) return st;
+    return launch_linear(ctx, layer, a);
+}
+
+static as_status check_history(as_ctx *ctx, const uint32_t *seen, int64_t seen_ld, const int32_t *counts, int64_t counts_ld,
+                               int64_t rows)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    if (rows < 0 || rows > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "rows outside [0, max_rows]");
+    if (rows == 0) return AS_OK;
+    if (!seen) return fail(ctx, AS_ERR_INVALID_ARG, "seen is NULL");
+    return check_record(ctx, seen, seen_ld, counts, counts_ld, ctx->V);
+}
+
+as_status as_history_set(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *counts, int64_t counts_ld, int64_t rows,
+                         const uint8_t *which, const int32_t *prompts, const int64_t *prompt_offsets, int64_t prompts_len,
+                         int32_t rows_per_prompt, const int32_t *tokens, int64_t tokens_ld, int32_t T, const int32_t *lens)
+{
+    const as_status st = check_history(ctx, seen, seen_ld, counts, counts_ld, rows);
+    if (st != AS_OK || rows == 0) return st;
+    if (prompts && (!prompt_offsets || prompts_len < 0 || rows_per_prompt < 1))
+        return fail(ctx, AS_ERR_INVALID_ARG, "prompts need prompt_offsets, prompts_len >= 0 and rows_per_prompt >= 1");
+    if (tokens && (T < 0 || tokens_ld < T)) return fail(ctx, AS_ERR_INVALID_ARG, "tokens need T >= 0 and tokens_ld >= T");
+    HistoryArgs a{};
+    a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V; a.which = which;
+    a.prompts = prompts; a.offsets = prompt_offsets; a.prompts_len = prompts_len; a.per = rows_per_prompt;
+    a.tokens = tokens; a.tokens_ld = tokens_ld; a.T = T; a.lens = lens;
+    return launch_history_set(ctx, a);
+}
+
+as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *counts, int64_t counts_ld, int64_t rows,
+                         const int32_t *tokens, const uint8_t *finished)
+{
+    const as_status st = check_history(ctx, seen, seen_ld, counts, counts_ld, rows);
+    if (st != AS_OK || rows == 0) return st;
+    if (!tokens) return fail(ctx, AS_ERR_INVALID_ARG, "tokens must not be NULL");
+    HistoryArgs a{};
+    a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V;
+    return launch_history_add(ctx, a, tokens, finished);
 }
 
 }  // extern "C"

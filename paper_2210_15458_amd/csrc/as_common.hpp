@@ -58,6 +58,7 @@ struct as_ctx {
     // encode workspace: the logits of a chunk of rows, the tables of a window of positions.  Its own, since encodes want
     // many rows where decodes of their size have few, and neither is to move the other's
     as::DeviceBuf encode_logits, encode_state;
+    as::DeviceBuf linear_x;        // as_linear: the rows of x that have to be laid out
     as::Profile prof;
     int step_shape = 0;            // work-group shape of the sampling kernel (tuning knob, 0 = default)
     // choices of a kernel (tuning knobs, 0 = by the rules on sizes)
@@ -79,6 +80,18 @@ struct as_model {
     as_dtype wdtype = AS_BF16;
     const void *E = nullptr;       // borrowed [V, d]
     void *Ut = nullptr;            // owned    [V, d]  (U transposed: K contiguous)
+};
+
+struct as_layer {
+    int32_t n = 0, k = 0;
+    as_dtype wdtype = AS_BF16;
+    as_act act = AS_ACT_NONE;
+    float act_arg = 0.f, scale = 1.f;
+    const void *W = nullptr;       // [n, ldw], borrowed or `own`
+    int64_t ldw = 0;
+    int32_t kp = 0;                // k, of a bf16 layer brought to a multiple of 64 (by zeros in W)
+    void *own = nullptr;           // the weights, where they had to be laid out
+    float *bias = nullptr;         // owned [n brought to a multiple of 256]
 };
 
 namespace as {
@@ -306,6 +319,50 @@ struct FusedArgs {
     const int32_t *prev;         // conditioning token of each row (may alias prev_out)
     int32_t *prev_out;
 };
+
+struct LinearArgs {
+    const void *x;               // [rows, ldx], the layer's wdtype
+    int64_t rows, ldx;
+    const void *W;               // [n, ldw]
+    int64_t ldw;
+    int32_t n, k;
+    // what follows the product
+    const float *bias;           // [n and more]: zeros where the layer has none
+    float scale;
+    int act;
+    float act_arg, act_inv;      // act_inv: 1 / act_arg
+    const void *residual;        // [rows, ldr] or null
+    int64_t ldr;
+    as_shaping shape;            // all members null: none
+    bool shaped;
+    void *out;                   // [rows, ldo]
+    int64_t ldo;
+    as_dtype out_dtype;
+};
+
+struct HistoryArgs {
+    uint32_t *seen;
+    int64_t seen_ld;
+    int32_t *counts;             // or null
+    int64_t counts_ld, rows;
+    int32_t V;
+    const uint8_t *which;        // or null
+    const int32_t *prompts;      // or null
+    const int64_t *offsets;
+    int64_t prompts_len;
+    int32_t per;                 // rows of a prompt
+    const int32_t *tokens;       // or null
+    int64_t tokens_ld;
+    int32_t T;
+    const int32_t *lens;         // or null
+};
+
+as_status launch_shape(as_ctx *ctx, const as_shaping &s, const void *logits, int64_t rows, int64_t ld, void *out, int64_t ldo);
+as_status launch_history_set(as_ctx *ctx, const HistoryArgs &a);
+as_status launch_history_add(as_ctx *ctx, const HistoryArgs &a, const int32_t *tokens, const uint8_t *finished);
+as_status launch_layer_layout(const as_layer &l, const void *W, int64_t ldw, const void *bias);
+size_t linear_workspace(const as_layer *l, const void *x, int64_t rows, int64_t ldx);
+as_status launch_linear(as_ctx *ctx, const as_layer *l, LinearArgs a);
 
 as_status launch_step(as_ctx *ctx, const StepArgs &a);
 as_status launch_fused_sample(as_ctx *ctx, const FusedArgs &a);
