@@ -7,8 +7,6 @@
 
 namespace as {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 // ---------------------------------------------------------------- epilogue
 
 // tanh x = 1 - 2 / (1 + e^2x), by its series below 1/4, where that difference would cancel (its next term is 8e-9 there)
@@ -42,25 +40,37 @@ __device__ __forceinline__ float activate(float z, int act, float arg, float inv
 template <class OutT>
 __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t row, int32_t col, float (&z)[8])
 {
-    const int left = a.n - col;
     const f32x4 b0 = *reinterpret_cast<const f32x4 *>(a.bias + col), b1 = *reinterpret_cast<const f32x4 *>(a.bias + col + 4);
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = activate(z[e] * a.scale + (e < 4 ? b0[e & 3] : b1[e & 3]), a.act, a.act_arg, a.act_inv);
-    if (a.residual) {
-        float add[8];
-        load8((const OutT *)a.residual + row * a.ldr + col, left, add);
+    if (a.shaped && a.shape.finished && a.shape.finished[row]) return;
+    const OutT *const add = (const OutT *)a.residual + row * a.ldr + col;
+    OutT *const to = (OutT *)a.out + row * a.ldo + col;
+    const int left = a.n - col;
+    if (left >= 8) {
+        if (a.residual) {
+            Raw8<OutT> raw;
+            float r[8];
+            load_raw8(add, raw);
+            widen8(raw, r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] += add[e];
+            for (int e = 0; e < 8; ++e) z[e] += r[e];
+        }
+        if (a.shaped) {
+            const ShapeRow r = shape_row<false>(a.shape, row);
+            Shape8 p;
+            shape8_request(r, col, p);
+            shape8_counts(r, col, p);
+            shape8_apply(r, col, p, z);
+        }
+        store8(to, z);
+    } else {
+        const ShapeRow r = shape_row<false>(a.shape, row);           // (nothing in it where there is no shaping)
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) store1(to + e, shape_one(r, col + e, a.residual ? z[e] + widen(add[e]) : z[e]));
     }
-    if (a.shaped) {
-        if (a.shape.finished && a.shape.finished[row]) return;
-        shape8(shape_row(a.shape, row), col, left, z);
-    }
-    store8((OutT *)a.out + row * a.ldo + col, left, z);
 }
-
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(uint16_t h) { return __builtin_bit_cast(float, (uint32_t)h << 16); }
 
 // ---------------------------------------------------------------- any product
 
