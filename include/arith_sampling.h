@@ -130,6 +130,8 @@ const char *as_last_error(const as_ctx *ctx);
  *                       4 = that is never done, the rest by choice; 5 = as
  *                       3, of the tokens that codes come to alone, made as
  *                       they do (weights as for 2, rows of one tile)
+ *   AS_TUNE_LINEAR_SHAPE  as_linear, bf16 layers: 1.. the tile of the output that
+ *                       a work-group takes, in the order of the source
  */
 typedef enum {
     AS_TUNE_STEP_SHAPE = 0,
@@ -137,7 +139,8 @@ typedef enum {
     AS_TUNE_THR_PATH = 2,
     AS_TUNE_GEMM_GM = 3,
     AS_TUNE_WORKSPACE_MIB = 4,
-    AS_TUNE_KEPT_ROWS = 5
+    AS_TUNE_KEPT_ROWS = 5,
+    AS_TUNE_LINEAR_SHAPE = 6
 } as_tuning;
 as_status as_ctx_set_tuning(as_ctx *ctx, as_tuning knob, int32_t value);
 

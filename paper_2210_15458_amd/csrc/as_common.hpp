@@ -68,6 +68,7 @@ struct as_ctx {
     int kept_rows = 0;             // decodes: 1 = no logits rows kept from step to step, 2 / 3 = kept / a table of all wherever there is room,
                                    // 4 = no table of all, 5 = one of the tokens that come
     int workspace_mib = 0;         // largest buffer of the workspace, in MiB (tuning knob: 0 = as large as the device gives)
+    int linear_shape = 0;          // as_linear: the tile of a block (tuning knob, 0 = by the rule on sizes)
     int num_cus = 0;               // compute units of the device (the persistent logits kernel runs one block on each)
     std::string err;
 };

@@ -137,6 +137,172 @@ __global__ __launch_bounds__(256) void linear_any(LinearArgs a, int32_t mtiles)
     }
 }
 
+// ---------------------------------------------------------------- tiles (bf16)
+
+// One block, four waves, a tile of TM x TN outputs.  The waves stand WM x WN x KG: KG groups share the tile's sum, group g
+// taking every KG-th of the K stages of 64, and add what they have in the epilogue, in the order of g.  So a product with few
+// tiles still has four waves on each, with that many more loads on their way, and no second launch to join them.
+//
+// Operands go global -> LDS directly (lane l's 16 bytes land at base + 16 l), 128 bytes of 8 rows a request, into a ring of
+// RING steps; LDS rows are 128 bytes with 16-byte piece c of row r at c ^ ((r >> 1) & 7), so that neither the fragment
+// reads nor the loads meet a bank twice.  Rows past either end repeat the last one and are not stored.
+// v_mfma_f32_32x32x16_bf16 with W as its first operand: register v of lane l is column 8 (v / 4) + 4 (l / 32) + v % 4 and
+// row l % 32 of the 32 x 32, so that a lane holds runs of four consecutive outputs.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void glb_void;
+constexpr int kStageK = 64;
+
+// the fragments of two K slices: all reads and their wait in one piece of text, so that nothing comes between a read in
+// flight and its register
+template <int FM, int FN> struct Frags {
+    bf16x8 w[2][FN], x[2][FM];
+};
+template <int FM, int FN>
+__device__ __forceinline__ void read_frags(Frags<FM, FN> &f, uint32_t w0, uint32_t x0, uint32_t w1, uint32_t x1)
+{
+    if constexpr (FM == 1 && FN == 1) {
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.w[0][0]), "=&v"(f.x[0][0]), "=&v"(f.w[1][0]), "=&v"(f.x[1][0])
+                     : "v"(w0), "v"(x0), "v"(w1), "v"(x1)
+                     : "memory");
+    } else if constexpr (FM == 2 && FN == 1) {
+        asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b128 %2, %7 offset:4096\n\t"
+                     "ds_read_b128 %3, %8\n\tds_read_b128 %4, %9\n\tds_read_b128 %5, %9 offset:4096\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.w[0][0]), "=&v"(f.x[0][0]), "=&v"(f.x[0][1]), "=&v"(f.w[1][0]), "=&v"(f.x[1][0]), "=&v"(f.x[1][1])
+                     : "v"(w0), "v"(x0), "v"(w1), "v"(x1)
+                     : "memory");
+    } else {
+        static_assert(FM == 2 && FN == 2, "the forms that there are");
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:4096\n\t"
+                     "ds_read_b128 %2, %9\n\tds_read_b128 %3, %9 offset:4096\n\t"
+                     "ds_read_b128 %4, %10\n\tds_read_b128 %5, %10 offset:4096\n\t"
+                     "ds_read_b128 %6, %11\n\tds_read_b128 %7, %11 offset:4096\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(f.w[0][0]), "=&v"(f.w[0][1]), "=&v"(f.x[0][0]), "=&v"(f.x[0][1]), "=&v"(f.w[1][0]), "=&v"(f.w[1][1]),
+                       "=&v"(f.x[1][0]), "=&v"(f.x[1][1])
+                     : "v"(w0), "v"(x0), "v"(w1), "v"(x1)
+                     : "memory");
+    }
+}
+
+template <class OutT, int WM, int WN, int KG, int FM, int FN, int RING>
+__global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles, uint32_t ntiles)
+{
+    static_assert(WM * WN * KG == 4 && (RING & (RING - 1)) == 0, "four waves; a ring of a power of two");
+    constexpr int TM = WM * FM * 32, TN = WN * FN * 32, kRows = TM + TN;
+    constexpr int kPart = kRows * 128, kStep = KG * kPart;            // bytes of a group's stage, of a step
+    constexpr int kPer = kRows / 32;                                  // requests of a wave for a group's stage
+    constexpr int kStride = TN + 4;                                   // floats of a staged row of sums
+    constexpr int kOut = KG * TM * kStride * 4;
+    constexpr int kLds = RING * kStep > kOut ? RING * kStep : kOut;
+    static_assert(kLds <= 160 * 1024 && (RING - 2) * kPer * KG < 64, "LDS, and what the wait can count");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kLds];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
+    // blocks of one column tile follow each other eight apart, on one XCD: its rows of W come through that L2 once
+    const uint32_t bid = blockIdx.x, eight = bid / (8 * mtiles), in = bid % (8 * mtiles);
+    const uint32_t across = ntiles - eight * 8 < 8 ? ntiles - eight * 8 : 8;
+    const int32_t n0 = (int32_t)((eight * 8 + in % across) * TN);
+    const int64_t m0 = (int64_t)(in / across) * TM;
+
+    // a wave's requests: rows i * 32 + wave * 8 + lane / 8 of the part, W's first
+    const int rl = wave * 8 + (lane >> 3);
+    const uint32_t piece = (uint32_t)(((lane & 7) ^ ((rl >> 1) & 7)) << 4);
+    const unsigned char *from[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int r = i * 32 + rl;
+        if (i * 32 < TN) {
+            const int32_t n = n0 + r < a.n ? n0 + r : a.n - 1;
+            from[i] = (const unsigned char *)a.W + (int64_t)n * a.ldw * 2 + piece;
+        } else {
+            const int64_t m = m0 + r - TN < a.rows ? m0 + r - TN : a.rows - 1;
+            from[i] = (const unsigned char *)a.x + m * a.ldx * 2 + piece;
+        }
+    }
+    const int stages = a.k / kStageK, steps = (stages + KG - 1) / KG;
+    auto request = [&](int step) __attribute__((always_inline)) {
+        unsigned char *const slot = smem + (step & (RING - 1)) * kStep + wave * 1024;
+#pragma unroll
+        for (int g = 0; g < KG; ++g) {
+            const int st = step * KG + g < stages ? step * KG + g : stages - 1;   // (past the end: loaded, not used)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                __builtin_amdgcn_global_load_lds((glb_void *)(from[i] + (int64_t)st * (kStageK * 2)),
+                                                 (lds_void *)(slot + g * kPart + i * 4096), 16, 0, 0);
+        }
+    };
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const int frow = lane & 31;
+    const uint32_t sw = (uint32_t)(((lane >> 5) ^ ((frow >> 1) & 7)) << 4);
+    const uint32_t fw = lds0 + kg * kPart + (uint32_t)(wn * FN * 32 + frow) * 128 + sw;
+    const uint32_t fx = lds0 + kg * kPart + (uint32_t)(TN + wm * FM * 32 + frow) * 128 + sw;
+    for (int s = 0; s < RING - 1 && s < steps; ++s) request(s);
+    for (int s = 0; s < steps; ++s) {
+        // step s has landed; up to RING - 2 more stay on their way
+        const int behind = steps - 1 - s;
+        if (behind >= RING - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 2) * kPer * KG) : "memory");
+        else if (RING > 3 && behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPer * KG) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // (every wave has left step s - 1, whose slot this is)
+        if (s + RING - 1 < steps) request(s + RING - 1);
+        if (KG > 1 && s * KG + kg >= stages) continue;
+        const uint32_t so = (uint32_t)(s & (RING - 1)) * kStep;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Frags<FM, FN> f;
+            read_frags<FM, FN>(f, (fw + so) ^ (uint32_t)(h * 64), (fx + so) ^ (uint32_t)(h * 64), (fw + so) ^ (uint32_t)(h * 64 + 32),
+                               (fx + so) ^ (uint32_t)(h * 64 + 32));
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[q][j], f.x[q][i], acc[i][j], 0, 0, 0);
+        }
+    }
+    __syncthreads();                                                  // the ring gives way to the sums
+    float *const sums = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4 *>(sums + (kg * TM + (wm * FM + i) * 32 + (lane & 31)) * kStride + (wn * FN + j) * 32 + 8 * q +
+                                           4 * (lane >> 5)) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __syncthreads();
+    for (int u = tid; u < TM * TN / 8; u += 256) {
+        const int r = u / (TN / 8), c = u % (TN / 8) * 8;
+        if (m0 + r >= a.rows || n0 + c >= a.n) continue;
+        float z[8];
+#pragma unroll
+        for (int g = 0; g < KG; ++g) {
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(sums + (g * TM + r) * kStride + c),
+                        hi = *reinterpret_cast<const f32x4 *>(sums + (g * TM + r) * kStride + c + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
+        }
+        finish8<OutT>(a, m0 + r, n0 + c, z);
+    }
+}
+
 // ---------------------------------------------------------------- layer
 
 // The layer's bias in fp32, zeros behind it up to a whole number of 256 columns (and everywhere, where it has none); and the
@@ -175,22 +341,62 @@ as_status launch_layer_layout(const as_layer &l, const void *W, int64_t ldw, con
 
 // ---------------------------------------------------------------- launch
 
+// Whether rows of x can be read as they are: whole pieces of 16 bytes, whole stages of K.
+static bool x_as_it_is(const as_layer *l, const void *x, int64_t ldx)
+{
+    return l->kp == l->k && ldx % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+}
+
 size_t linear_workspace(const as_layer *l, const void *x, int64_t rows, int64_t ldx)
 {
-    return 0;
+    return l->wdtype == AS_BF16 && !x_as_it_is(l, x, ldx) ? (size_t)rows * l->kp * 2 : 0;
+}
+
+template <class OutT, int WM, int WN, int KG, int FM, int FN, int RING> static as_status launch_tile(as_ctx *ctx, const LinearArgs &a)
+{
+    constexpr int TM = WM * FM * 32, TN = WN * FN * 32;
+    const int64_t mtiles = (a.rows + TM - 1) / TM, ntiles = (a.n + TN - 1) / TN;
+    if (mtiles * ntiles > 0x7fffffffLL || mtiles > 0x0fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "product too large for one launch");
+    launch(ctx, kKernelLogits, linear_tile<OutT, WM, WN, KG, FM, FN, RING>, dim3((unsigned)(mtiles * ntiles)), dim3(256), 0, a,
+           (uint32_t)mtiles, (uint32_t)ntiles);
+    return AS_OK;
+}
+
+template <class OutT> static as_status launch_bf16(as_ctx *ctx, const LinearArgs &a)
+{
+    switch (ctx->linear_shape) {
+    case 1: return launch_tile<OutT, 1, 1, 4, 1, 1, 4>(ctx, a);      // 32 x 32, four groups
+    case 2: return launch_tile<OutT, 1, 2, 2, 1, 1, 4>(ctx, a);      // 32 x 64, two groups
+    case 3: return launch_tile<OutT, 1, 4, 1, 1, 1, 4>(ctx, a);      // 32 x 128
+    case 4: return launch_tile<OutT, 1, 4, 1, 2, 1, 4>(ctx, a);      // 64 x 128
+    case 5: return launch_tile<OutT, 2, 2, 1, 2, 2, 4>(ctx, a);      // 128 x 128
+    case 6: return launch_tile<OutT, 1, 1, 4, 2, 2, 2>(ctx, a);      // 64 x 64, four groups
+    case 7: return launch_tile<OutT, 1, 2, 2, 2, 1, 4>(ctx, a);      // 64 x 64, two groups
+    case 8: return launch_tile<OutT, 2, 2, 1, 1, 1, 4>(ctx, a);      // 64 x 64
+    }
+    return launch_tile<OutT, 1, 4, 1, 1, 1, 4>(ctx, a);
 }
 
 as_status launch_linear(as_ctx *ctx, const as_layer *l, LinearArgs a)
 {
-    const int64_t mtiles = (a.rows + 63) / 64, blocks = mtiles * ((a.n + 63) / 64);
-    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "product too large for one launch");
-    const dim3 grid((unsigned)blocks);
-    if (l->wdtype == AS_F32)
-        launch(ctx, kKernelLogits, linear_any<float, float>, grid, dim3(256), 0, a, (int32_t)mtiles);
-    else if (a.out_dtype == AS_BF16)
-        launch(ctx, kKernelLogits, linear_any<uint16_t, uint16_t>, grid, dim3(256), 0, a, (int32_t)mtiles);
-    else
-        launch(ctx, kKernelLogits, linear_any<uint16_t, float>, grid, dim3(256), 0, a, (int32_t)mtiles);
+    as_status st = AS_OK;
+    if (l->wdtype == AS_F32) {
+        const int64_t mtiles = (a.rows + 63) / 64, blocks = mtiles * ((a.n + 63) / 64);
+        if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "product too large for one launch");
+        launch(ctx, kKernelLogits, linear_any<float, float>, dim3((unsigned)blocks), dim3(256), 0, a, (int32_t)mtiles);
+    } else {
+        if (!x_as_it_is(l, a.x, a.ldx)) {
+            const int64_t blocks = (a.rows * l->kp + 255) / 256;
+            if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "x too large to lay out");
+            hipLaunchKernelGGL(layout_kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, (const uint16_t *)a.x, a.ldx, a.rows,
+                               l->k, (uint16_t *)ctx->linear_x.ptr, l->kp);
+            a.x = ctx->linear_x.ptr;
+            a.ldx = l->kp;
+        }
+        a.k = l->kp;
+        st = a.out_dtype == AS_BF16 ? launch_bf16<uint16_t>(ctx, a) : launch_bf16<float>(ctx, a);
+    }
+    if (st != AS_OK) return st;
     AS_HIP_TRY(ctx, hipGetLastError());
     return AS_OK;
 }
