@@ -19,36 +19,69 @@ __device__ __forceinline__ float tanh_of(float x)
     return fabsf(x) < 0.25f ? s : copysignf(t, x);
 }
 
-__device__ __forceinline__ float activate(float z, int act, float arg, float inv)
+// The same in fewer steps: (1 - t) / (1 + t), t = e^-2|x|, whose difference is 2^-23 / 2|x| off, and two terms of the series
+// below 1/32: at most 2e-6 off, a thousandth of the rounding to bf16 that follows.
+__device__ __forceinline__ float tanh_for_bf16(float x)
+{
+    const float t = __builtin_amdgcn_exp2f(-2.88539008177792681472f * fabsf(x));
+    const float y = copysignf((1.f - t) * __builtin_amdgcn_rcpf(1.f + t), x);
+    return fabsf(x) < 0.03125f ? fmaf(x * (-1.f / 3.f), x * x, x) : y;
+}
+
+// erf by Abramowitz and Stegun 7.1.26 (1.5e-7 off at most): erfc x = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x >= 0.
+// z/2 (1 + erf(z / sqrt 2)) = z h or z (1 - h) with h = erfc(|z| / sqrt 2) / 2: no cancellation in the lower tail.
+__device__ __forceinline__ float gelu_of(float z)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, fabsf(z), 1.f));
+    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170368f * (z * z));
+    const float c = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f), 0.5f * 1.421413741f),
+                                     -0.5f * 0.284496736f), 0.5f * 0.254829592f);
+    const float h = c * e;
+    return z * (z > 0.f ? 1.f - h : h);
+}
+
+// The activation of N sums: the choice once, outside.
+template <class OutT, int N, class V> __device__ __forceinline__ void activate(V &z, int act, float arg, float inv)
 {
     switch (act) {
-    case AS_ACT_RELU: return z < 0.f ? 0.f : z;                       // (NaN stays)
-    case AS_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752440f));
-    // z/2 (1 + tanh u) = z / (1 + e^-2u)
-    case AS_ACT_GELU_TANH: {
-        const float u = z * (0.79788456080286535588f + 0.79788456080286535588f * 0.044715f * z * z);
-        return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.88539008177792681472f * u));
-    }
-    case AS_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
-    case AS_ACT_SOFTCAP: return arg * tanh_of(z * inv);
-    default: return z;
+    case AS_ACT_RELU:
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = z[e] < 0.f ? 0.f : z[e];   // (NaN stays)
+        break;
+    case AS_ACT_GELU:
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = gelu_of(z[e]);
+        break;
+    case AS_ACT_GELU_TANH:                                            // z/2 (1 + tanh u) = z / (1 + e^-2u)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float u = z[e] * (0.79788456080286535588f + 0.79788456080286535588f * 0.044715f * z[e] * z[e]);
+            z[e] = z[e] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.88539008177792681472f * u));
+        }
+        break;
+    case AS_ACT_SILU:
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = z[e] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z[e]));
+        break;
+    case AS_ACT_SOFTCAP:
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = arg * (sizeof(OutT) == 2 ? tanh_for_bf16(z[e] * inv) : tanh_of(z[e] * inv));
+        break;
     }
 }
 
-// Eight sums of one row, columns col .. col + 7 (col a multiple of 8 below n): everything behind the product, in fp32, with
+// Eight outputs of one row, columns col .. col + 7 (col a multiple of 8 below n): what follows the activation, in fp32, with
 // one rounding at the store.
-template <class OutT>
+template <class OutT, bool RESIDUAL = true, bool SHAPED = true>
 __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t row, int32_t col, float (&z)[8])
 {
-    const f32x4 b0 = *reinterpret_cast<const f32x4 *>(a.bias + col), b1 = *reinterpret_cast<const f32x4 *>(a.bias + col + 4);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = activate(z[e] * a.scale + (e < 4 ? b0[e & 3] : b1[e & 3]), a.act, a.act_arg, a.act_inv);
-    if (a.shaped && a.shape.finished && a.shape.finished[row]) return;
+    const bool shaped = SHAPED && a.shaped, more = RESIDUAL && a.residual;
+    if (shaped && a.shape.finished && a.shape.finished[row]) return;
     const OutT *const add = (const OutT *)a.residual + row * a.ldr + col;
     OutT *const to = (OutT *)a.out + row * a.ldo + col;
     const int left = a.n - col;
     if (left >= 8) {
-        if (a.residual) {
+        if (more) {
             Raw8<OutT> raw;
             float r[8];
             load_raw8(add, raw);
@@ -56,7 +89,7 @@ __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t row, int32_
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] += r[e];
         }
-        if (a.shaped) {
+        if (shaped) {
             const ShapeRow r = shape_row<false>(a.shape, row);
             Shape8 p;
             shape8_request(r, col, p);
@@ -65,11 +98,25 @@ __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t row, int32_
         }
         store8(to, z);
     } else {
-        const ShapeRow r = shape_row<false>(a.shape, row);           // (nothing in it where there is no shaping)
 #pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < left) store1(to + e, shape_one(r, col + e, a.residual ? z[e] + widen(add[e]) : z[e]));
+        for (int e = 0; e < 7; ++e) {
+            if (e >= left) continue;
+            float y = more ? z[e] + widen(add[e]) : z[e];
+            if (shaped) y = shape_one(shape_row<false>(a.shape, row), col + e, y);
+            store1(to + e, y);
+        }
     }
+}
+
+// The same from the sums.
+template <class OutT>
+__device__ __forceinline__ void finish8_sums(const LinearArgs &a, int64_t row, int32_t col, float (&z)[8])
+{
+    const f32x4 b0 = *reinterpret_cast<const f32x4 *>(a.bias + col), b1 = *reinterpret_cast<const f32x4 *>(a.bias + col + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], a.scale, e < 4 ? b0[e & 3] : b1[e & 3]);
+    activate<OutT, 8>(z, a.act, a.act_arg, a.act_inv);
+    finish8<OutT>(a, row, col, z);
 }
 
 // ---------------------------------------------------------------- any product
@@ -133,7 +180,7 @@ __global__ __launch_bounds__(256) void linear_any(LinearArgs a, int32_t mtiles)
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = lds[r * kOut + c + e];
-        finish8<OutT>(a, m0 + r, n0 + c, z);
+        finish8_sums<OutT>(a, m0 + r, n0 + c, z);
     }
 }
 
@@ -299,8 +346,585 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
         }
-        finish8<OutT>(a, m0 + r, n0 + c, z);
+        finish8_sums<OutT>(a, m0 + r, n0 + c, z);
     }
+}
+
+// ---------------------------------------------------------------- large products (bf16)
+
+// A block of 8 waves (4 x 2, each 64 x 128 of 256 x 256 outputs) a compute unit, which walks its tiles; the load stream is two
+// stages of 64 k ahead of the products and runs on across tile ends, so that only the epilogue's own time stands between two
+// tiles.  A stage of 64 KB is requested whole, a request or two between two matrix instructions, into the slot of the ring
+// that the stage before last has just left.  Fragments are read by hand, one between every two matrix instructions, a slice
+// of 16 k ahead; the schedule is pinned.
+//
+// Tiles stand in bands of eight rows of tiles, and the columns of a band go to the 8 XCDs in turn, as the blocks do: what the 32
+// workers of an XCD have open at a time, 8 row and 4 column tiles, comes into its L2 once, and the XCDs write side by side.
+constexpr int kBigM = 256, kBigN = 256;
+constexpr int kBigX = kBigM * kStageK * 2, kBigRing = (kBigM + kBigN) * kStageK * 2;       // 32 KB of x rows in a stage of 64 KB
+constexpr int kBigStage = 4096;                                                            // a wave's own, for the epilogue
+constexpr int kBigLds = 2 * kBigRing + 8 * kBigStage;                                      // all of a compute unit's 160 KB
+
+template <int OFFSET> __device__ __forceinline__ bf16x8 lds_read8(uint32_t at)
+{
+    bf16x8 r;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(at), "n"(OFFSET));
+    return r;
+}
+
+// A wave's 64 x 128 outputs shaped.  What the rows say of them (strengths, table rows, bits) is requested into the wave's LDS while
+// the products run, one word of each row a lane, and taken from there when the sums are done.  The seen columns, few as a rule
+// and anywhere, are then listed in that LDS and dealt out, kDealt a lane, so that their counts come in one go; each lane
+// puts its penalties on the sums where they lie turned in LDS (32 x 32 of them at a time), and biases and masks follow,
+// eight columns a lane.  Where more are seen (the first columns of a vocabulary ordered by frequency) the counts of all
+// columns are read, eight a lane: as many bytes as that many lines.
+constexpr int kDealt = 2;                     // seen columns of 32 x 128, a lane
+constexpr uint32_t kOfRows = 512, kOfBits = kOfRows + 5 * 256;       // in the wave's LDS, behind the bias
+
+// Requests of a tile's rows m .. m + 63 and columns n .. n + 127.
+__device__ __forceinline__ void request_rows(const LinearArgs &a, unsigned char *stage, int64_t m, int32_t n, int lane)
+{
+    const as_shaping &s = a.shape;
+    const int64_t row = m + lane < a.rows ? m + lane : a.rows - 1;
+    auto word = [&](const void *p, uint32_t at) __attribute__((always_inline)) {
+        __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(stage + at), 4, 0, 0);
+    };
+    if (s.repetition) word(s.repetition + row, kOfRows);
+    if (s.presence) word(s.presence + row, kOfRows + 256);
+    if (s.frequency) word(s.frequency + row, kOfRows + 512);
+    if (s.bias_ids) word(s.bias_ids + row, kOfRows + 768);
+    if (s.mask_ids) word(s.mask_ids + row, kOfRows + 1024);
+    if (s.seen) {
+        const int32_t words = (a.n + 31) >> 5;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int32_t w = (n >> 5) + e < words ? (n >> 5) + e : words - 1;
+            word(s.seen + row * s.seen_ld + w, kOfBits + e * 256);
+        }
+    }
+}
+
+// What a lane (row b of either 32, half h of the columns) has of that.
+struct ShapeTile {
+    float repetition[2], inverse[2], presence[2], frequency[2];
+    int32_t bias[2];                          // the row of the table, -1: none, -2: the row is not to be written
+    uint32_t seen[2][2], mask[2][2];          // words 2h and 2h + 1
+    int total[2];                             // seen columns of the wave's 32 rows; if dealt out:
+    int32_t place[2][kDealt];                 // row * 128 + column, or -1
+    float less[2][kDealt];                    // what it is to lose
+};
+
+__device__ __forceinline__ uint32_t lds_word(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds_float(uint32_t at) { return __builtin_bit_cast(float, lds_word(at)); }
+__device__ __forceinline__ int32_t table_row(int64_t id, int64_t rows) { return (int32_t)(id < rows ? id : rows - 1); }
+
+__device__ __forceinline__ void take_rows(const LinearArgs &a, ShapeTile &t, uint32_t stage, int64_t m, int32_t n, int lane)
+{
+    const as_shaping &s = a.shape;
+    const int b = lane & 31, h = lane >> 5;
+    const int32_t words = (a.n + 31) >> 5;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t row = m + i * 32 + b, last = a.rows - 1, mine = row < last ? row : last;
+        const uint32_t at = stage + (uint32_t)(i * 32 + b) * 4;
+        t.repetition[i] = s.repetition ? lds_float(at + kOfRows) : 1.f;
+        t.presence[i] = s.presence ? lds_float(at + kOfRows + 256) : 0.f;
+        t.frequency[i] = s.frequency ? lds_float(at + kOfRows + 512) : 0.f;
+        t.inverse[i] = 1.f / t.repetition[i];
+        t.bias[i] = -1;
+        if (s.bias) {
+            t.bias[i] = table_row(s.bias_ids ? (int32_t)lds_word(at + kOfRows + 768) : s.bias_rows == 1 ? 0 : mine, s.bias_rows);
+            t.bias[i] = t.bias[i] < 0 ? -1 : t.bias[i];
+        }
+        const bool done = row > last || (s.finished && s.finished[mine]);
+        if (done) t.bias[i] = -2;
+        int32_t id = -1;
+        if (s.mask) id = table_row(s.mask_ids ? (int32_t)lds_word(at + kOfRows + 1024) : s.mask_rows == 1 ? 0 : mine, s.mask_rows);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int32_t word = (n >> 5) + 2 * h + e, left = a.n - word * 32;
+            t.mask[i][e] = id < 0 ? 0xffffffffu : s.mask[id * s.mask_ld + (word < words ? word : words - 1)];
+            t.seen[i][e] = s.seen && !done ? lds_word(at + kOfBits + (2 * h + e) * 256) : 0u;
+            if (left < 32) t.seen[i][e] &= left > 0 ? (1u << left) - 1u : 0u;
+        }
+    }
+    if (!s.seen) return;
+    int32_t count[2][kDealt];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int mine = __popc(t.seen[i][0]) + __popc(t.seen[i][1]);
+        const int upto = (int)wave_scan_add((float)mine);
+        t.total[i] = __builtin_amdgcn_readlane(upto, 63);
+        if (t.total[i] > kDealt * kWave) continue;
+        uint32_t at = stage + i * 1024 + (uint32_t)(upto - mine) * 4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            for (uint32_t w = t.seen[i][e]; w; w &= w - 1, at += 4)
+                asm volatile("ds_write_b32 %0, %1" ::"v"(at), "v"(b * 128 + (2 * h + e) * 32 + __ffs((int)w) - 1) : "memory");
+#pragma unroll
+        for (int k = 0; k < kDealt; ++k) {
+            t.place[i][k] = -1;
+            count[i][k] = 0;
+            if (k * kWave >= t.total[i]) continue;                    // (the same for the whole wave)
+            const int32_t p = (int32_t)lds_word(stage + i * 1024 + (uint32_t)(k * kWave + lane) * 4);
+            if (k * kWave + lane < t.total[i]) t.place[i][k] = p;
+            if (s.counts && t.place[i][k] >= 0)
+                count[i][k] = s.counts[(m + i * 32 + (p >> 7)) * s.counts_ld + n + (p & 127)];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < kDealt; ++k) {
+            if (t.total[i] > kDealt * kWave || k * kWave >= t.total[i]) continue;
+            const int from = t.place[i][k] >= 0 ? t.place[i][k] >> 7 : 0;
+            ShapeRow of;
+            of.frequency = __shfl(t.frequency[i], from, kWave);
+            of.presence = __shfl(t.presence[i], from, kWave);
+            t.less[i][k] = lost(of, count[i][k]);
+        }
+}
+
+// The half of it that is rows m .. m + 31, sums `acc` (lane b + 32 h has row b), to memory.
+template <class OutT, int I>
+__device__ __forceinline__ void shape_sums(const LinearArgs &a, const ShapeTile &t, f32x16 (&acc)[4], uint32_t stage, int64_t m, int32_t n, int lane)
+{
+    const as_shaping &s = a.shape;
+    const int b = lane & 31, h = lane >> 5;
+    const bool dealt = t.total[I] <= kDealt * kWave;
+    // where the lane's eight columns of the turned sums come from: row lane / 4 and the one 16 on
+    const int row = lane >> 2, c = (lane & 3) * 2;
+    int32_t bias[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) bias[p] = __shfl(t.bias[I], p * 16 + row, kWave);
+    f32x4 add[2][2];
+    i32x4_any count[2][2];
+    // what the lane needs of its columns of 32 x 32 number j
+    auto ahead = [&](int j) __attribute__((always_inline)) {
+        const int32_t col = n + j * 32 + c * 4;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            if (s.bias) {
+                add[p][0] = add[p][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float *const from = s.bias + bias[p] * s.bias_ld + col;
+                if (bias[p] >= 0 && col + 8 <= a.n) {
+                    add[p][0] = *reinterpret_cast<const f32x4_any *>(from);
+                    add[p][1] = *reinterpret_cast<const f32x4_any *>(from + 4);
+                } else if (bias[p] >= 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (col + e < a.n) add[p][e >> 2][e & 3] = from[e];
+                }
+            }
+            if (s.counts && !dealt) {
+                const int32_t *const from = s.counts + (m + p * 16 + row) * s.counts_ld + col;
+                if (bias[p] != -2 && col + 8 <= a.n) {
+                    count[p][0] = *reinterpret_cast<const i32x4_any *>(from);
+                    count[p][1] = *reinterpret_cast<const i32x4_any *>(from + 4);
+                } else if (bias[p] != -2) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (col + e < a.n) count[p][e >> 2][e & 3] = from[e];
+                }
+            }
+        }
+    };
+    ahead(0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 w = {acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
+            asm volatile("ds_write_b128 %0, %1" ::"v"(stage + b * 128 + (((q * 2 + h) ^ (b & 7)) << 4)), "v"(w) : "memory");
+        }
+        if (s.seen && dealt) {
+#pragma unroll
+            for (int k = 0; k < kDealt; ++k) {
+                if (k * kWave >= t.total[I]) continue;
+                const int32_t place = t.place[I][k];
+                const int pr = place >= 0 ? place >> 7 : 0, pc = place & 31;
+                const float up = __shfl(t.inverse[I], pr, kWave), down = __shfl(t.repetition[I], pr, kWave);
+                if (place < 0 || (place & 127) >> 5 != j) continue;
+                const uint32_t at = stage + pr * 128 + (((pc >> 2) ^ (pr & 7)) << 4) + (pc & 3) * 4;
+                float y = lds_float(at);
+                y = fmaf(y, y > 0.f ? up : down, -t.less[I][k]);
+                asm volatile("ds_write_b32 %0, %1" ::"v"(at), "v"(y) : "memory");
+            }
+        }
+        f32x4 v[4];
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                     : "v"(stage + row * 128 + ((c ^ (row & 7)) << 4)), "v"(stage + row * 128 + (((c + 1) ^ (row & 7)) << 4))
+                     : "memory");
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int from = p * 16 + row, word = from + 32 * (j >> 1);
+            if (s.seen && !dealt) {
+                const uint32_t bits = (uint32_t)__shfl((int)t.seen[I][j & 1], word, kWave) >> ((lane & 3) * 8);
+                ShapeRow of;
+                of.frequency = __shfl(t.frequency[I], from, kWave);
+                of.presence = __shfl(t.presence[I], from, kWave);
+                of.inverse = __shfl(t.inverse[I], from, kWave);
+                of.repetition = __shfl(t.repetition[I], from, kWave);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = v[2 * p + (e >> 2)][e & 3];
+                    v[2 * p + (e >> 2)][e & 3] = shape1(of, bits >> e & 1u, s.counts ? count[p][e >> 2][e & 3] : 0, 0.f, true, y);
+                }
+            }
+            if (s.bias) {
+                v[2 * p] += add[p][0];
+                v[2 * p + 1] += add[p][1];
+            }
+            if (s.mask) {
+                const uint32_t free = (uint32_t)__shfl((int)t.mask[I][j & 1], word, kWave) >> ((lane & 3) * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[2 * p + (e >> 2)][e & 3] = free >> e & 1u ? v[2 * p + (e >> 2)][e & 3] : -__builtin_inff();
+            }
+        }
+        if (j < 3) ahead(j + 1);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            float z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = v[2 * p + (e >> 2)][e & 3];
+            const int32_t col = n + j * 32 + c * 4, left = a.n - col;
+            if (bias[p] == -2 || left <= 0) continue;
+            OutT *const to = (OutT *)a.out + (m + p * 16 + row) * a.ldo + col;
+            if (left >= 8) {
+                store8(to, z);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) store1(to + e, z[e]);
+            }
+        }
+    }
+}
+
+// The epilogue of a wave's 64 x 128: bias and activation where the sums are, then turned through the wave's own 4 KB of LDS, so
+// that a lane holds eight consecutive columns of a row.  With nothing further to do bf16 outputs are turned as such, 32 x 64
+// at a time, and written in whole lines; fp32 outputs, and those that have a residual or a shaping before they are rounded,
+// 32 x 32 at a time.  16-byte piece c of the 128 bytes of LDS row r lies at c ^ (r & 7).  The LDS accesses are written by hand, so
+// that the compiler does not tie them to the requests in flight.
+template <class OutT, int FORM>
+__device__ __forceinline__ int big_epilogue(const LinearArgs &a, f32x16 (&acc)[2][4], uint32_t stage, int64_t m, int32_t n, int lane)
+{
+    asm volatile("" : "+v"(lane));           // (its addresses are worked out here: kept over the products they would not fit)
+    const int b = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f32x4 add[4];                        // (the bias lies in the wave's LDS)
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\tds_read_b128 %3, %4 offset:96\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(add[0]), "=&v"(add[1]), "=&v"(add[2]), "=&v"(add[3])
+                     : "v"(stage + j * 128 + h * 16)
+                     : "memory");
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = fmaf(acc[i][j][4 * q + e], a.scale, add[q][e]);
+    }
+    [[maybe_unused]] ShapeTile tile;         // (its loads are on their way while the activation is worked out)
+    if constexpr (FORM == 2) take_rows(a, tile, stage, m, n, lane);
+    if (a.act != AS_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f32x4 t = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    activate<OutT, 4>(t, a.act, a.act_arg, a.act_inv);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = t[e];
+                    __builtin_amdgcn_sched_barrier(0);                // (not more at a time than there are registers for)
+                }
+    }
+    const bool inside = m + 64 <= a.rows && n + 128 <= a.n;
+    if constexpr (FORM == 0 && sizeof(OutT) == 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int ps = 0; ps < 2; ++ps) {
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16 &t = acc[i][ps * 2 + jj];
+                        const uint64_t w = (uint64_t)pack2_bf16(t[4 * q + 2], t[4 * q + 3]) << 32 | pack2_bf16(t[4 * q], t[4 * q + 1]);
+                        asm volatile("ds_write_b64 %0, %1" ::"v"(stage + b * 128 + (((jj * 4 + q) ^ (b & 7)) << 4) + h * 8), "v"(w)
+                                     : "memory");
+                    }
+                // a lane's pieces are of rows 8 apart, in one column of pieces
+                const int row = lane >> 3;
+                const uint32_t at = stage + row * 128 + (((lane & 7) ^ row) << 4);
+                u32x4_any val[4];
+                asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_b128 %2, %4 offset:2048\n\t"
+                             "ds_read_b128 %3, %4 offset:3072\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(val[0]), "=&v"(val[1]), "=&v"(val[2]), "=&v"(val[3])
+                             : "v"(at)
+                             : "memory");
+                const int64_t r = m + i * 32 + row;
+                const int32_t col = n + ps * 64 + (lane & 7) * 8;
+                OutT *to = (OutT *)a.out + r * a.ldo + col;
+#pragma unroll
+                for (int p = 0; p < 4; ++p, to += 8 * a.ldo) {
+                    if (inside) {
+                        *reinterpret_cast<u32x4_any *>(to) = val[p];
+                    } else if (r + p * 8 < a.rows) {
+                        if (col + 8 <= a.n) {
+                            *reinterpret_cast<u32x4_any *>(to) = val[p];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 7; ++e) {
+                                const uint32_t w = val[p][e >> 1];
+                                if (col + e < a.n) to[e] = (OutT)(w >> ((e & 1) * 16));
+                            }
+                        }
+                    }
+                }
+            }
+        return inside ? 16 : -1;
+    } else if constexpr (FORM == 2) {
+        shape_sums<OutT, 0>(a, tile, acc[0], stage, m, n, lane);
+        shape_sums<OutT, 1>(a, tile, acc[1], stage, m + 32, n, lane);
+        // (loads that were waited for meanwhile only leave less behind)
+        return inside && __all(tile.bias[0] != -2 && tile.bias[1] != -2) ? 8 * (int)sizeof(OutT) : -1;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 w = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    asm volatile("ds_write_b128 %0, %1" ::"v"(stage + b * 128 + (((q * 2 + h) ^ (b & 7)) << 4)), "v"(w) : "memory");
+                }
+                const int row = lane >> 2, c = (lane & 3) * 2;        // (and the row 16 on, of the same swizzle)
+                f32x4 t[4];
+                asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
+                             "s_waitcnt lgkmcnt(0)"
+                             : "=&v"(t[0]), "=&v"(t[1]), "=&v"(t[2]), "=&v"(t[3])
+                             : "v"(stage + row * 128 + ((c ^ (row & 7)) << 4)), "v"(stage + row * 128 + (((c + 1) ^ (row & 7)) << 4))
+                             : "memory");
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    float z[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = t[2 * p + (e >> 2)][e & 3];
+                    const int64_t r = m + i * 32 + p * 16 + row;
+                    const int32_t col = n + j * 32 + c * 4;
+                    if (FORM == 0 && inside) store8((OutT *)a.out + r * a.ldo + col, z);
+                    else if (r < a.rows && col < a.n) finish8<OutT, FORM == 1, false>(a, r, col, z);
+                }
+            }
+        return FORM == 0 && inside ? 32 : -1;
+    }
+}
+
+// FORM: what follows the activation, 0 nothing, 1 a residual, 2 a shaping.
+template <class OutT, int FORM>
+__global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtiles, uint32_t ntiles)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kBigLds];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const uint32_t x = blockIdx.x & 7, q = blockIdx.x >> 3, W = gridDim.x >> 3;
+    const uint32_t high = mtiles < 8 ? mtiles : 8, low = mtiles % high, bands = mtiles / high;      // the last band has `low` rows of tiles
+    const uint32_t columns = bands * ntiles, here = columns > x ? (columns - x + 7) / 8 : 0;        // of whole height; on this XCD
+    const uint32_t x2 = (x - columns) & 7, here2 = low && ntiles > x2 ? (ntiles - x2 + 7) / 8 : 0;  // of the last band
+    const uint32_t all = here * high + here2 * low;
+    if (q >= all) return;
+    const uint32_t tiles = (all - q + W - 1) / W;
+    auto place = [&](uint32_t j, int64_t &m0, int32_t &n0) __attribute__((always_inline)) {
+        uint32_t t = q + j * W;
+        if (t < here * high) {
+            const uint32_t c = x + 8 * (t / high), band = c / ntiles;
+            m0 = (int64_t)(band * high + t % high) * kBigM;
+            n0 = (int32_t)((c - band * ntiles) * kBigN);
+        } else {
+            t -= here * high;
+            m0 = (int64_t)(bands * high + t % low) * kBigM;
+            n0 = (int32_t)((x2 + 8 * (t / low)) * kBigN);
+        }
+    };
+
+    // requests: chunk it * 8 + wave of a stage, it 0..3 rows it * 64 + rowb of x, it 4..7 of W; addresses are a uniform base and
+    // a lane's 32-bit offset, which changes with the tile only where it has less than 256 rows
+    const int rowb = wave * 8 + (lane >> 3);
+    const uint32_t piece = (uint32_t)(((lane & 7) ^ ((rowb >> 1) & 7)) << 4);
+    const unsigned char *xbase = nullptr, *wbase = nullptr;           // of the tile that is being requested
+    uint32_t xoff[4], woff[4];
+    auto aim = [&](int64_t m0, int32_t n0) __attribute__((always_inline)) {
+        xbase = (const unsigned char *)a.x + m0 * a.ldx * 2;
+        wbase = (const unsigned char *)a.W + (int64_t)n0 * a.ldw * 2;
+        const int mleft = a.rows - m0 < kBigM ? (int)(a.rows - m0) : kBigM, nleft = a.n - n0 < kBigN ? a.n - n0 : kBigN;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 64 + rowb;
+            xoff[it] = (uint32_t)(r < mleft ? r : mleft - 1) * (uint32_t)(a.ldx * 2) + piece;
+            woff[it] = (uint32_t)(r < nleft ? r : nleft - 1) * (uint32_t)(a.ldw * 2) + piece;
+        }
+    };
+    const int nstages = a.k / kStageK;                                // at least two
+    uint32_t jload = 0;                                               // the tile, and its stage, that is requested next
+    int sload = 0;
+    auto request1 = [&](int slot, auto it_c) __attribute__((always_inline)) {
+        constexpr int it = decltype(it_c)::value;
+        unsigned char *const dst = smem + slot * kBigRing + (it * 8 + wave) * 1024;
+        if constexpr (it < 4)
+            __builtin_amdgcn_global_load_lds((glb_void *)(xbase + (int64_t)sload * (kStageK * 2) + xoff[it]), (lds_void *)dst, 16, 0, 0);
+        else
+            __builtin_amdgcn_global_load_lds((glb_void *)(wbase + (int64_t)sload * (kStageK * 2) + woff[it - 4]), (lds_void *)dst, 16, 0, 0);
+    };
+    auto requested = [&]() __attribute__((always_inline)) {           // a whole stage has been: on to the next
+        if (++sload == nstages) {
+            sload = 0;
+            if (++jload < tiles) {
+                int64_t m0;
+                int32_t n0;
+                place(jload, m0, n0);
+                aim(m0, n0);
+            }
+        }
+    };
+
+    f32x16 acc[2][4];
+    const int frow = lane & 31, fc = lane >> 5;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    // (32 rows on are 4 KB on: the swizzle is the same)
+    const uint32_t fx = lds0 + (wm * 64 + frow) * 128 + ((fc ^ ((frow >> 1) & 7)) << 4);
+    const uint32_t fw = lds0 + kBigX + (wn * 128 + frow) * 128 + ((fc ^ ((frow >> 1) & 7)) << 4);
+#define AS_SB() __builtin_amdgcn_sched_barrier(0)
+#define AS_RQ(slot_, n_)                                                                                    \
+    do {                                                                                                    \
+        request1(slot_, std::integral_constant<int, n_>{});                                                 \
+        AS_SB();                                                                                            \
+    } while (0)
+#define AS_RX(f_, i_, so_, kk_)                                                                             \
+    do {                                                                                                    \
+        f_[i_] = lds_read8<(i_) * 4096>((fx + (so_)) ^ ((kk_) << 5));                                               \
+        AS_SB();                                                                                            \
+    } while (0)
+#define AS_RW(f_, j_, so_, kk_)                                                                             \
+    do {                                                                                                    \
+        f_[j_] = lds_read8<(j_) * 4096>((fw + (so_)) ^ ((kk_) << 5));                                               \
+        AS_SB();                                                                                            \
+    } while (0)
+#define AS_MM(x_, w_, i_, j_)                                                                               \
+    do {                                                                                                    \
+        acc[i_][j_] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w_[j_], x_[i_], acc[i_][j_], 0, 0, 0);        \
+        AS_SB();                                                                                            \
+    } while (0)
+    // the fragments are outputs of hand-written reads: the wait is tied to them, so that no product moves above it
+#define AS_WAIT(x_, w_)                                                                                     \
+    do {                                                                                                    \
+        asm volatile("s_waitcnt lgkmcnt(0)"                                                                 \
+                     : "+v"(x_[0]), "+v"(x_[1]), "+v"(w_[0]), "+v"(w_[1]), "+v"(w_[2]), "+v"(w_[3]));       \
+        AS_SB();                                                                                            \
+    } while (0)
+    // multiply the slice in (x_, w_) while slice kk_ is read into (nx_, nw_)
+#define AS_SLICE(x_, w_, nx_, nw_, so_, kk_)                                                                \
+    do {                                                                                                    \
+        AS_RX(nx_, 0, so_, kk_); AS_MM(x_, w_, 0, 0); AS_RW(nw_, 0, so_, kk_); AS_MM(x_, w_, 0, 1);         \
+        AS_RW(nw_, 1, so_, kk_); AS_MM(x_, w_, 0, 2); AS_RX(nx_, 1, so_, kk_); AS_MM(x_, w_, 0, 3);         \
+        AS_RW(nw_, 2, so_, kk_); AS_MM(x_, w_, 1, 0); AS_RW(nw_, 3, so_, kk_); AS_MM(x_, w_, 1, 1);         \
+        AS_MM(x_, w_, 1, 2); AS_MM(x_, w_, 1, 3);                                                           \
+    } while (0)
+
+    int64_t m0;
+    int32_t n0;
+    place(0, m0, n0);
+    aim(m0, n0);
+    AS_RQ(0, 0); AS_RQ(0, 1); AS_RQ(0, 2); AS_RQ(0, 3); AS_RQ(0, 4); AS_RQ(0, 5); AS_RQ(0, 6); AS_RQ(0, 7);
+    requested();
+    AS_RQ(1, 0); AS_RQ(1, 1); AS_RQ(1, 2); AS_RQ(1, 3); AS_RQ(1, 4); AS_RQ(1, 5); AS_RQ(1, 6); AS_RQ(1, 7);
+    requested();
+    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");                  // stage 0 has landed, stage 1 may still fly
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    bf16x8 xa[2], wa[4], xb[2], wb[4];
+    AS_RX(xa, 0, 0u, 0); AS_RX(xa, 1, 0u, 0);
+    AS_RW(wa, 0, 0u, 0); AS_RW(wa, 1, 0u, 0); AS_RW(wa, 2, 0u, 0); AS_RW(wa, 3, 0u, 0);
+    int gs = 0;                                                       // stages worked on: stage gs lies in slot gs & 1
+    int stores = 0;                                                   // of the tile before, behind the requests for this one
+    for (uint32_t j = 0; j < tiles; ++j) {
+        place(j, m0, n0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][jj][v] = 0.f;
+        for (int s = 0; s < nstages; ++s, ++gs) {
+            const int cur = gs & 1;
+            const uint32_t so = (uint32_t)cur * kBigRing, son = (uint32_t)(cur ^ 1) * kBigRing;
+            const bool more = jload < tiles;
+            AS_WAIT(xa, wa);
+            AS_SLICE(xa, wa, xb, wb, so, 1);
+            AS_WAIT(xb, wb);
+            AS_SLICE(xb, wb, xa, wa, so, 2);
+            AS_WAIT(xa, wa);
+            AS_SLICE(xa, wa, xb, wb, so, 3);
+            AS_WAIT(xb, wb);
+            // every wave has read all of this stage, and the next one has landed; the stores of the tile before, which were
+            // requested after it, may drain on
+            if (s == 0 && stores == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+            else if (s == 0 && stores == 32) asm volatile("s_waitcnt vmcnt(32)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            AS_SB();
+            // the bias of the wave's columns, to where the epilogue finds it: landed before the second stage ends
+            if (s == 0) {
+                const float *const bias = a.bias + n0 + wn * 128 + lane;
+                __builtin_amdgcn_global_load_lds((glb_void *)bias, (lds_void *)(smem + 2 * kBigRing + wave * kBigStage), 4, 0, 0);
+                __builtin_amdgcn_global_load_lds((glb_void *)(bias + 64), (lds_void *)(smem + 2 * kBigRing + wave * kBigStage + 256), 4, 0, 0);
+                if constexpr (FORM == 2) request_rows(a, smem + 2 * kBigRing + wave * kBigStage, m0 + wm * 64, n0 + wn * 128, lane);
+                AS_SB();
+            }
+            // the last slice, with the first fragments of the next stage (read for nothing behind the last of all) and the requests
+            // of the one after it
+            AS_RX(xa, 0, son, 0); AS_MM(xb, wb, 0, 0);
+            AS_RW(wa, 0, son, 0); AS_MM(xb, wb, 0, 1);
+            if (more) AS_RQ(cur, 0);
+            AS_RW(wa, 1, son, 0); AS_MM(xb, wb, 0, 2);
+            if (more) AS_RQ(cur, 1);
+            AS_RX(xa, 1, son, 0); AS_MM(xb, wb, 0, 3);
+            if (more) AS_RQ(cur, 2);
+            AS_RW(wa, 2, son, 0); AS_MM(xb, wb, 1, 0);
+            if (more) AS_RQ(cur, 3);
+            AS_RW(wa, 3, son, 0); AS_MM(xb, wb, 1, 1);
+            if (more) { AS_RQ(cur, 4); AS_RQ(cur, 5); }
+            AS_MM(xb, wb, 1, 2);
+            if (more) { AS_RQ(cur, 6); AS_RQ(cur, 7); }
+            AS_MM(xb, wb, 1, 3);
+            if (more) requested();
+        }
+        AS_WAIT(xa, wa);                                              // (in flight they must not meet other code)
+        stores = big_epilogue<OutT, FORM>(a, acc, lds0 + 2 * kBigRing + (uint32_t)wave * kBigStage, m0 + wm * 64, n0 + wn * 128, lane);
+        // the first fragments of the next tile, again: they do not take the epilogue's registers
+        const uint32_t so = (uint32_t)(gs & 1) * kBigRing;
+        AS_RX(xa, 0, so, 0); AS_RX(xa, 1, so, 0);
+        AS_RW(wa, 0, so, 0); AS_RW(wa, 1, so, 0); AS_RW(wa, 2, so, 0); AS_RW(wa, 3, so, 0);
+    }
+#undef AS_SB
+#undef AS_RQ
+#undef AS_RX
+#undef AS_RW
+#undef AS_MM
+#undef AS_WAIT
+#undef AS_SLICE
 }
 
 // ---------------------------------------------------------------- layer
@@ -362,8 +986,26 @@ template <class OutT, int WM, int WN, int KG, int FM, int FN, int RING> static a
     return AS_OK;
 }
 
+template <class OutT> static as_status launch_big(as_ctx *ctx, const LinearArgs &a)
+{
+    const uint32_t mtiles = (uint32_t)((a.rows + kBigM - 1) / kBigM), ntiles = (uint32_t)((a.n + kBigN - 1) / kBigN);
+    const dim3 grid((unsigned)(ctx->num_cus / 8 * 8));
+    if (a.shaped) launch(ctx, kKernelLogits, linear_big<OutT, 2>, grid, dim3(512), 0, a, mtiles, ntiles);
+    else if (a.residual) launch(ctx, kKernelLogits, linear_big<OutT, 1>, grid, dim3(512), 0, a, mtiles, ntiles);
+    else launch(ctx, kKernelLogits, linear_big<OutT, 0>, grid, dim3(512), 0, a, mtiles, ntiles);
+    return AS_OK;
+}
+
+// Whether the kernel for large products can take it: two stages of K, 32-bit offsets inside a tile.
+static bool big_applies(const as_ctx *ctx, const LinearArgs &a)
+{
+    return a.k >= 2 * kStageK && ctx->num_cus >= 8 && a.ldx < (1 << 22) && a.ldw < (1 << 22) &&
+           (a.rows + kBigM - 1) / kBigM * ((a.n + kBigN - 1) / kBigN) < (1LL << 30);
+}
+
 template <class OutT> static as_status launch_bf16(as_ctx *ctx, const LinearArgs &a)
 {
+    if (ctx->linear_shape == 9 && big_applies(ctx, a) && !(a.shaped && a.residual)) return launch_big<OutT>(ctx, a);
     switch (ctx->linear_shape) {
     case 1: return launch_tile<OutT, 1, 1, 4, 1, 1, 4>(ctx, a);      // 32 x 32, four groups
     case 2: return launch_tile<OutT, 1, 2, 2, 1, 1, 4>(ctx, a);      // 32 x 64, two groups
