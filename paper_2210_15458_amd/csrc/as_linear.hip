@@ -184,6 +184,57 @@ __global__ __launch_bounds__(256) void linear_any(LinearArgs a, int32_t mtiles)
     }
 }
 
+// What a thread finishes, eight columns of a row, whose own loads go out in two rounds, beside the products where they can:
+// what the row and the columns say, and what that points to.
+template <class OutT> struct Unit {
+    int64_t row;
+    int32_t col;
+    bool whole;                               // all eight inside
+    Raw8<OutT> add;
+    ShapeRow r;
+    Shape8 p;
+
+    __device__ __forceinline__ void first(const LinearArgs &a)
+    {
+        whole = row < a.rows && col + 8 <= a.n;
+        if (!whole) return;
+        if (a.residual) load_raw8((const OutT *)a.residual + row * a.ldr + col, add);
+        if (a.shaped) {
+            r = shape_row<false>(a.shape, row);
+            if (r.seen) p.seen = r.seen[col >> 5];
+        }
+    }
+    __device__ __forceinline__ void second(const LinearArgs &a)
+    {
+        if (!whole || !a.shaped) return;
+        if (r.mask) p.mask = r.mask[col >> 5];
+        if (r.bias) {
+            p.bias[0] = *reinterpret_cast<const f32x4_any *>(r.bias + col);
+            p.bias[1] = *reinterpret_cast<const f32x4_any *>(r.bias + col + 4);
+        }
+        shape8_counts(r, col, p);
+    }
+    __device__ __forceinline__ void finish(const LinearArgs &a, const f32x4 (&bias)[2], float (&z)[8])
+    {
+        if (row >= a.rows || col >= a.n) return;
+        if (!whole) return finish8_sums<OutT>(a, row, col, z);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = fmaf(z[e], a.scale, bias[e >> 2][e & 3]);
+        activate<OutT, 8>(z, a.act, a.act_arg, a.act_inv);
+        if (a.residual) {
+            float y[8];
+            widen8(add, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] += y[e];
+        }
+        if (a.shaped) {
+            if (a.shape.finished && a.shape.finished[row]) return;
+            shape8_apply(r, col, p, z);
+        }
+        store8((OutT *)a.out + row * a.ldo + col, z);
+    }
+};
+
 // ---------------------------------------------------------------- tiles (bf16)
 
 // One block, four waves, a tile of TM x TN outputs.  The waves stand WM x WN x KG: KG groups share the tile's sum, group g
@@ -239,7 +290,7 @@ __device__ __forceinline__ void read_frags(Frags<FM, FN> &f, uint32_t w0, uint32
 template <class OutT, int WM, int WN, int KG, int FM, int FN, int RING>
 __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles, uint32_t ntiles)
 {
-    static_assert(WM * WN * KG == 4 && (RING & (RING - 1)) == 0, "four waves; a ring of a power of two");
+    static_assert(WM * WN * KG == 4 && RING >= 2, "four waves; a slot to work on and one to fill");
     constexpr int TM = WM * FM * 32, TN = WN * FN * 32, kRows = TM + TN;
     constexpr int kPart = kRows * 128, kStep = KG * kPart;            // bytes of a group's stage, of a step
     constexpr int kPer = kRows / 32;                                  // requests of a wave for a group's stage
@@ -273,8 +324,10 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
         }
     }
     const int stages = a.k / kStageK, steps = (stages + KG - 1) / KG;
+    int fill = 0;                                                     // the slot of the next step to request
     auto request = [&](int step) __attribute__((always_inline)) {
-        unsigned char *const slot = smem + (step & (RING - 1)) * kStep + wave * 1024;
+        unsigned char *const slot = smem + fill * kStep + wave * 1024;
+        fill = fill == RING - 1 ? 0 : fill + 1;
 #pragma unroll
         for (int g = 0; g < KG; ++g) {
             const int st = step * KG + g < stages ? step * KG + g : stages - 1;   // (past the end: loaded, not used)
@@ -296,19 +349,38 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
     const uint32_t sw = (uint32_t)(((lane >> 5) ^ ((frow >> 1) & 7)) << 4);
     const uint32_t fw = lds0 + kg * kPart + (uint32_t)(wn * FN * 32 + frow) * 128 + sw;
     const uint32_t fx = lds0 + kg * kPart + (uint32_t)(TN + wm * FM * 32 + frow) * 128 + sw;
+    // what a thread finishes: always the same eight columns, of rows 256 / kAcross apart
+    constexpr int kAcross = TN / 8, kUnits = TM * kAcross > 256 ? TM * kAcross / 256 : 1, kAhead = kUnits < 2 ? 1 : 2;
+    Unit<OutT> unit[kAhead];
+    f32x4 bias[2] = {};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int r = u * (256 / kAcross) + tid / kAcross;
+        unit[u].row = r < TM ? m0 + r : a.rows;
+        unit[u].col = n0 + tid % kAcross * 8;
+        unit[u].first(a);
+    }
+    if (unit[0].col < a.n) {
+        bias[0] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col);
+        bias[1] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col + 4);
+    }
     for (int s = 0; s < RING - 1 && s < steps; ++s) request(s);
-    for (int s = 0; s < steps; ++s) {
+    for (int s = 0, slot_of = 0; s < steps; ++s, slot_of = slot_of == RING - 1 ? 0 : slot_of + 1) {
         // step s has landed; up to RING - 2 more stay on their way
         const int behind = steps - 1 - s;
         if (behind >= RING - 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 2) * kPer * KG) : "memory");
-        else if (RING > 3 && behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPer * KG) : "memory");
+        else if (RING > 6 && behind >= 4) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kPer * KG) : "memory");
+        else if (RING > 4 && behind >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kPer * KG) : "memory");
+        else if (RING > 3 && behind >= 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPer * KG) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // (every wave has left step s - 1, whose slot this is)
-        if (s + RING - 1 < steps) request(s + RING - 1);
-        if (KG > 1 && s * KG + kg >= stages) continue;
-        const uint32_t so = (uint32_t)(s & (RING - 1)) * kStep;
+        // (every wave has left step s - 1, whose slot is filled: at once where nothing else is on its way, and where something is
+        // behind the first products, which then need not wait for the requests to be taken)
+        const bool more = s + RING - 1 < steps, idle = KG > 1 && s * KG + kg >= stages;
+        if (more && (RING == 2 || idle)) request(s + RING - 1);
+        if (idle) continue;
+        const uint32_t so = (uint32_t)slot_of * kStep;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             Frags<FM, FN> f;
@@ -321,8 +393,11 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[q][j], f.x[q][i], acc[i][j], 0, 0, 0);
+            if (RING > 2 && h == 0 && more) request(s + RING - 1);
         }
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) unit[u].second(a);
     __syncthreads();                                                  // the ring gives way to the sums
     float *const sums = reinterpret_cast<float *>(smem);
 #pragma unroll
@@ -335,19 +410,102 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
                                            4 * (lane >> 5)) =
                     f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     __syncthreads();
-    for (int u = tid; u < TM * TN / 8; u += 256) {
-        const int r = u / (TN / 8), c = u % (TN / 8) * 8;
-        if (m0 + r >= a.rows || n0 + c >= a.n) continue;
-        float z[8];
+    for (int u0 = 0; u0 < kUnits; u0 += kAhead) {
+        if (u0 > 0) {
 #pragma unroll
-        for (int g = 0; g < KG; ++g) {
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(sums + (g * TM + r) * kStride + c),
-                        hi = *reinterpret_cast<const f32x4 *>(sums + (g * TM + r) * kStride + c + 4);
+            for (int u = 0; u < kAhead; ++u) {
+                unit[u].row += kAhead * (256 / kAcross);
+                unit[u].first(a);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
+            for (int u = 0; u < kAhead; ++u) unit[u].second(a);
         }
-        finish8_sums<OutT>(a, m0 + r, n0 + c, z);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = (u0 + u) * (256 / kAcross) + tid / kAcross;
+            if (TM * kAcross < 256 && r >= TM) continue;
+            float z[8];
+#pragma unroll
+            for (int g = 0; g < KG; ++g) {
+                const float *const at = sums + (g * TM + r) * kStride + tid % kAcross * 8;
+                const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
+            }
+            unit[u].finish(a, bias, z);
+        }
     }
+}
+
+// ---------------------------------------------------------------- few rows (bf16)
+
+// Up to 16 rows: a pass over W, each of whose elements one wave needs once, so that LDS would be a detour.  A wave takes 16 columns
+// (v_mfma_f32_16x16x32_bf16, W first: lane l has 8 k from 8 (l / 16) on of row l % 16, and of the result row l % 16, columns
+// 4 (l / 16) .. + 3) and one of KW shares of the sum, with U stages of 64 k, whole lines, on their way at once; the shares meet in
+// LDS, in order.  WAVES / KW column groups a block.
+template <class OutT, int WAVES, int KW, int U>
+__global__ __launch_bounds__(WAVES * kWave) void linear_few(LinearArgs a)
+{
+    constexpr int WN = WAVES / KW, kStride = WN * 16 + 4, kUnits = 16 * WN * 2;
+    static_assert(kUnits <= WAVES * kWave, "a unit a thread");
+    __shared__ __attribute__((aligned(16))) float sums[KW * 16 * kStride];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = wave / WN, wn = wave % WN, l = lane & 15, quarter = lane >> 4;
+    const int32_t n0 = (int32_t)blockIdx.x * (WN * 16), mine = n0 + wn * 16 + l;
+    const unsigned char *const w = (const unsigned char *)a.W + (int64_t)(mine < a.n ? mine : a.n - 1) * a.ldw * 2 + quarter * 16;
+    const unsigned char *const x = (const unsigned char *)a.x + (l < a.rows ? l : a.rows - 1) * a.ldx * 2 + quarter * 16;
+    const int stages = a.k / kStageK, from = stages * kg / KW, to = stages * (kg + 1) / KW;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    bf16x8 fw[U][2], fx[U][2];
+    auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u >= to) break;
+            const int64_t at = (int64_t)(s0 + u) * (kStageK * 2);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                fw[u][h] = *reinterpret_cast<const bf16x8 *>(w + at + h * 64);
+                fx[u][h] = *reinterpret_cast<const bf16x8 *>(x + at + h * 64);
+            }
+        }
+    };
+    auto multiply = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u >= to) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[u][h], fx[u][h], acc, 0, 0, 0);
+        }
+    };
+    Unit<OutT> unit;
+    unit.row = tid < kUnits ? tid / (WN * 2) : a.rows;
+    unit.col = n0 + tid % (WN * 2) * 8;
+    f32x4 bias[2] = {};
+    if (from < to) load(from);
+    unit.first(a);
+    if (unit.col < a.n) {
+        bias[0] = *reinterpret_cast<const f32x4 *>(a.bias + unit.col);
+        bias[1] = *reinterpret_cast<const f32x4 *>(a.bias + unit.col + 4);
+    }
+    if (from < to) multiply(from);
+    unit.second(a);
+    for (int s0 = from + U; s0 < to; s0 += U) {
+        load(s0);
+        multiply(s0);
+    }
+    *reinterpret_cast<f32x4 *>(sums + (kg * 16 + l) * kStride + wn * 16 + quarter * 4) = acc;
+    __syncthreads();
+    if (tid >= kUnits) return;
+    float z[8];
+#pragma unroll
+    for (int g = 0; g < KW; ++g) {
+        const float *const at = sums + (g * 16 + tid / (WN * 2)) * kStride + tid % (WN * 2) * 8;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
+    }
+    unit.finish(a, bias, z);
 }
 
 // ---------------------------------------------------------------- large products (bf16)
@@ -986,6 +1144,13 @@ template <class OutT, int WM, int WN, int KG, int FM, int FN, int RING> static a
     return AS_OK;
 }
 
+template <class OutT, int WAVES, int KW, int U> static as_status launch_few(as_ctx *ctx, const LinearArgs &a)
+{
+    constexpr int TN = WAVES / KW * 16;
+    launch(ctx, kKernelLogits, linear_few<OutT, WAVES, KW, U>, dim3((unsigned)((a.n + TN - 1) / TN)), dim3(WAVES * kWave), 0, a);
+    return AS_OK;
+}
+
 template <class OutT> static as_status launch_big(as_ctx *ctx, const LinearArgs &a)
 {
     const uint32_t mtiles = (uint32_t)((a.rows + kBigM - 1) / kBigM), ntiles = (uint32_t)((a.n + kBigN - 1) / kBigN);
@@ -999,24 +1164,73 @@ template <class OutT> static as_status launch_big(as_ctx *ctx, const LinearArgs 
 // Whether the kernel for large products can take it: two stages of K, 32-bit offsets inside a tile.
 static bool big_applies(const as_ctx *ctx, const LinearArgs &a)
 {
-    return a.k >= 2 * kStageK && ctx->num_cus >= 8 && a.ldx < (1 << 22) && a.ldw < (1 << 22) &&
+    return a.k >= 2 * kStageK && ctx->num_cus >= 8 && !(a.shaped && a.residual) && a.ldx < (1 << 22) && a.ldw < (1 << 22) &&
            (a.rows + kBigM - 1) / kBigM * ((a.n + kBigN - 1) / kBigN) < (1LL << 30);
+}
+
+// Which form a product takes: the least of these times, in us, with S stages of 64 k, lines fitted to the launches below on 256
+// compute units; where the wide ones differ little their order does not matter.  A tile of 32 x 32 whose four waves share the
+// sum has the shortest way through a long one; with two blocks a compute unit (Many) it takes more tiles; 64 x 64 has
+// less traffic, alone with more on its way, or five blocks a unit; 128 x 128 and the large one less again.
+//            rows k n      32   32 Many  64   64 Many  128   large
+//      64  512   2048     3.8    3.7    5.1    4.9    9.4   18.7
+//      64 1024   8192     9.4    6.2    7.5   10.5   14.3   27.8
+//     128 2048   2048     7.7    8.0   11.0   17.0   24.4   44.7
+//     256 1024   4096    17.2   10.7    7.8   10.5   15.9   28.2
+//    1024 2048    512    14.5    9.7   11.3   17.5   24.6   45.4
+//    1024  512   2048    23.5   14.2    7.6    7.8   11.8   19.8
+//    2048  512   2048    44.4   25.4   13.3   12.0   13.1   20.6
+//    2048 2048   2048    99.8   78.2   36.3   32.4   29.1   47.1
+//     128  512  32128    44.7   25.8   13.8   12.6   13.9   22.2
+//    1024  512  32128     390    235   94.4   83.2   93.5   50
+//    4096 1024   4096     249    168   84.0   68.6   73.4   41.0
+// A shaping adds to what a block does behind its sums: 256 x 512 x 32128 39.1 / 29.4 / 53.2 / 45.4 (64, 64 Many, 128, large), 1024 x
+// 512 x 32128 153 / 117 / 211 / 92.
+// Up to 16 rows (us, by 2, 4 and 8 shares of the sum, then 32 Many and 64 Many): 1 x 512 x 2048 3.1 / 3.1 / 4.5 / 3.6 / 4.5, 1 x
+// 512 x 8192 3.8 / 4.7 / 7.3 / 4.6 / 6.3, 1 x 4096 x 4096 16.2 / 9.5 / 8.1 / 13.8 / 29.9, 16 x 2048 x 512 9.0 / 5.8 / 5.9 / 6.3 / 9.9, 1 x
+// 1024 x 256000 85.2 / 78.8 / 152 / 97.3 / 88.9, 16 x 512 x 32128 9.6 / 16.7 / 31.5 / 9.3 / 7.6, 16 x 1024 x 256000 127 / 126 / 230 / 111 / 95.4:
+// many rows over many columns read x once too often.
+enum Form { kByRule, kTile32, kTile32Many, kTile64, kTile64Many, kTile128, kBig, kFew2, kFew4, kFew8, kForms };
+
+static Form form_of(const as_ctx *ctx, const LinearArgs &a)
+{
+    if (ctx->linear_shape > kByRule && ctx->linear_shape < kForms) {
+        const Form f = (Form)ctx->linear_shape;
+        const bool can = f == kBig ? big_applies(ctx, a) : f < kFew2 || a.rows <= 16;
+        if (can) return f;
+    }
+    const double S = (double)a.k / kStageK, cus = ctx->num_cus > 0 ? ctx->num_cus : 1;
+    if (a.rows <= 4 || (a.rows <= 16 && a.n <= 8192)) return S >= 48 ? kFew8 : S >= 16 || a.n <= 4096 ? kFew4 : kFew2;
+    auto units = [&](int64_t t) { return ceil((double)((a.rows + t - 1) / t) * (double)((a.n + t - 1) / t) / cus); };      // tiles a compute unit
+    const double u32 = units(32), u64 = units(64), u128 = units(128), u256 = units(256), more = a.shaped ? 1.0 : 0.0;
+    const double few = u64 < 5 ? u64 : 5, full = (double)((a.rows + 255) / 256) * (double)((a.n + 255) / 256) / cus;
+    const double t[] = {
+        1.2 + u32 * (1.2 + 0.16 * S),
+        1.2 + (u32 <= 1 ? 0.7 : ceil(u32 / 2)) * (0.9 + 0.26 * S),
+        2.6 + 0.26 * S + (u64 - 1) * (0.9 + 0.235 * S) + more * (4.5 + 1.85 * u64),
+        2.2 + 0.46 * S + (few - 1) * (0.6 + 0.14 * S) + (u64 - few) * (0.75 + 0.225 * S) + more * (4.0 + u64),
+        1.0 + u128 * (7.2 + 0.6 * S + 15.0 * more),
+        5.0 + u256 * (4.0 + 1.1 * S + 0.7 * S * (full < 1 ? full : 1) + 20.0 * more),
+    };
+    int best = 0;
+    for (int f = 1; f < 6; ++f)
+        if (t[f] < t[best] && (f < 5 || big_applies(ctx, a))) best = f;
+    return (Form)(best + 1);
 }
 
 template <class OutT> static as_status launch_bf16(as_ctx *ctx, const LinearArgs &a)
 {
-    if (ctx->linear_shape == 9 && big_applies(ctx, a) && !(a.shaped && a.residual)) return launch_big<OutT>(ctx, a);
-    switch (ctx->linear_shape) {
-    case 1: return launch_tile<OutT, 1, 1, 4, 1, 1, 4>(ctx, a);      // 32 x 32, four groups
-    case 2: return launch_tile<OutT, 1, 2, 2, 1, 1, 4>(ctx, a);      // 32 x 64, two groups
-    case 3: return launch_tile<OutT, 1, 4, 1, 1, 1, 4>(ctx, a);      // 32 x 128
-    case 4: return launch_tile<OutT, 1, 4, 1, 2, 1, 4>(ctx, a);      // 64 x 128
-    case 5: return launch_tile<OutT, 2, 2, 1, 2, 2, 4>(ctx, a);      // 128 x 128
-    case 6: return launch_tile<OutT, 1, 1, 4, 2, 2, 2>(ctx, a);      // 64 x 64, four groups
-    case 7: return launch_tile<OutT, 1, 2, 2, 2, 1, 4>(ctx, a);      // 64 x 64, two groups
-    case 8: return launch_tile<OutT, 2, 2, 1, 1, 1, 4>(ctx, a);      // 64 x 64
+    switch (form_of(ctx, a)) {
+    case kTile32: return launch_tile<OutT, 1, 1, 4, 1, 1, 4>(ctx, a);
+    case kTile32Many: return launch_tile<OutT, 1, 1, 4, 1, 1, 2>(ctx, a);
+    case kTile64: return launch_tile<OutT, 2, 2, 1, 1, 1, 4>(ctx, a);
+    case kTile128: return launch_tile<OutT, 2, 2, 1, 2, 2, 4>(ctx, a);
+    case kBig: return launch_big<OutT>(ctx, a);
+    case kFew2: return launch_few<OutT, 4, 2, 4>(ctx, a);
+    case kFew4: return launch_few<OutT, 4, 4, 4>(ctx, a);
+    case kFew8: return launch_few<OutT, 8, 8, 4>(ctx, a);
+    default: return launch_tile<OutT, 2, 2, 1, 1, 1, 2>(ctx, a);
     }
-    return launch_tile<OutT, 1, 4, 1, 1, 1, 4>(ctx, a);
 }
 
 as_status launch_linear(as_ctx *ctx, const as_layer *l, LinearArgs a)
