@@ -130,8 +130,12 @@ const char *as_last_error(const as_ctx *ctx);
  *                       4 = that is never done, the rest by choice; 5 = as
  *                       3, of the tokens that codes come to alone, made as
  *                       they do (weights as for 2, rows of one tile)
- *   AS_TUNE_LINEAR_SHAPE  as_linear, bf16 layers: 1.. the tile of the output that
- *                       a work-group takes, in the order of the source
+ *   AS_TUNE_LINEAR_SHAPE  as_linear: the form of its kernel where that can take the
+ *                       product.  bf16 layers: 1, 2 = 32 x 32 of the output
+ *                       a work-group (for few, many of them), 3, 4 = 64 x 64 the
+ *                       same, 5 = 128 x 128, 6 = 256 x 256, 7, 8, 9 = up to 16
+ *                       rows, in 2, 4, 8 shares of the sum; fp32 layers: 1..5 =
+ *                       16 x 16, 16 x 32, 32 x 64, 64 x 64, 128 x 128
  */
 typedef enum {
     AS_TUNE_STEP_SHAPE = 0,

@@ -119,71 +119,6 @@ __device__ __forceinline__ void finish8_sums(const LinearArgs &a, int64_t row, i
     finish8<OutT>(a, row, col, z);
 }
 
-// ---------------------------------------------------------------- any product
-
-// 64 x 64 of the output a block, 32 k at a time through LDS, v_mfma_f32_16x16x4_f32: lane l holds k = l / 16 of row l % 16
-// of either operand, and of the result column l % 16 and rows 4 (l / 16) .. + 3.
-template <class T, class OutT>
-__global__ __launch_bounds__(256) void linear_any(LinearArgs a, int32_t mtiles)
-{
-    constexpr int KS = 32, kStride = KS + 4, kOut = 64 + 4;
-    __shared__ __attribute__((aligned(16))) float lds[2 * 64 * kStride > 64 * kOut ? 2 * 64 * kStride : 64 * kOut];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t m0 = (int64_t)(blockIdx.x % mtiles) * 64;
-    const int32_t n0 = (int32_t)(blockIdx.x / mtiles) * 64;
-    const T *x = (const T *)a.x, *W = (const T *)a.W;
-    f32x4 acc[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int wm = wave >> 1, wn = wave & 1;
-    for (int32_t k0 = 0; k0 < a.k; k0 += KS) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int u = tid + i * 256, r = u / KS, k = k0 + u % KS;          // rows 0..63 of x, 64..127 of W
-            float v = 0.f;
-            if (r < 64) {
-                if (m0 + r < a.rows && k < a.k) v = widen(x[(m0 + r) * a.ldx + k]);
-            } else if (n0 + r - 64 < a.n && k < a.k) {
-                v = widen(W[(int64_t)(n0 + r - 64) * a.ldw + k]);
-            }
-            lds[r * kStride + u % KS] = v;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < KS; kk += 4) {
-            float fa[2], fb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = lds[(wm * 32 + i * 16 + (lane & 15)) * kStride + kk + (lane >> 4)];
-                fb[i] = lds[(64 + wn * 32 + i * 16 + (lane & 15)) * kStride + kk + (lane >> 4)];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                lds[(wm * 32 + i * 16 + 4 * (lane >> 4) + v) * kOut + wn * 32 + j * 16 + (lane & 15)] = acc[i][j][v];
-    __syncthreads();
-    for (int u = tid; u < 64 * 8; u += 256) {
-        const int r = u >> 3, c = (u & 7) * 8;
-        if (m0 + r >= a.rows || n0 + c >= a.n) continue;
-        float z[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = lds[r * kOut + c + e];
-        finish8_sums<OutT>(a, m0 + r, n0 + c, z);
-    }
-}
-
 // What a thread finishes, eight columns of a row, whose own loads go out in two rounds, beside the products where they can:
 // what the row and the columns say, and what that points to.
 template <class OutT> struct Unit {
@@ -232,6 +167,65 @@ template <class OutT> struct Unit {
             shape8_apply(r, col, p, z);
         }
         store8((OutT *)a.out + row * a.ldo + col, z);
+    }
+};
+
+// What 256 threads finish of a tile of TM x TN: each always the same eight columns, of rows 256 / kAcross apart; two of them have
+// their loads out beside the products.  The sums lie in LDS, KG shares of TM rows, kStride floats apart, added in order.
+template <class OutT, int TM, int TN, int KG> struct TileEnd {
+    static constexpr int kAcross = TN / 8, kUnits = TM * kAcross > 256 ? TM * kAcross / 256 : 1, kAhead = kUnits < 2 ? 1 : 2;
+    static constexpr int kStride = TN + 4, kBytes = KG * TM * kStride * 4;
+    Unit<OutT> unit[kAhead];
+    f32x4 bias[2];
+
+    __device__ __forceinline__ void first(const LinearArgs &a, int64_t m0, int32_t n0)
+    {
+        const int tid = threadIdx.x;
+        bias[0] = bias[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = u * (256 / kAcross) + tid / kAcross;
+            unit[u].row = r < TM ? m0 + r : a.rows;
+            unit[u].col = n0 + tid % kAcross * 8;
+            unit[u].first(a);
+        }
+        if (unit[0].col < a.n) {
+            bias[0] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col);
+            bias[1] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col + 4);
+        }
+    }
+    __device__ __forceinline__ void second(const LinearArgs &a)
+    {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) unit[u].second(a);
+    }
+    __device__ __forceinline__ void finish(const LinearArgs &a, const float *sums)
+    {
+        const int tid = threadIdx.x;
+        for (int u0 = 0; u0 < kUnits; u0 += kAhead) {
+            if (u0 > 0) {
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    unit[u].row += kAhead * (256 / kAcross);
+                    unit[u].first(a);
+                }
+                second(a);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int r = (u0 + u) * (256 / kAcross) + tid / kAcross;
+                if (TM * kAcross < 256 && r >= TM) continue;
+                float z[8];
+#pragma unroll
+                for (int g = 0; g < KG; ++g) {
+                    const float *const at = sums + (g * TM + r) * kStride + tid % kAcross * 8;
+                    const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
+                }
+                unit[u].finish(a, bias, z);
+            }
+        }
     }
 };
 
@@ -294,8 +288,7 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
     constexpr int TM = WM * FM * 32, TN = WN * FN * 32, kRows = TM + TN;
     constexpr int kPart = kRows * 128, kStep = KG * kPart;            // bytes of a group's stage, of a step
     constexpr int kPer = kRows / 32;                                  // requests of a wave for a group's stage
-    constexpr int kStride = TN + 4;                                   // floats of a staged row of sums
-    constexpr int kOut = KG * TM * kStride * 4;
+    constexpr int kOut = TileEnd<OutT, TM, TN, KG>::kBytes;
     constexpr int kLds = RING * kStep > kOut ? RING * kStep : kOut;
     static_assert(kLds <= 160 * 1024 && (RING - 2) * kPer * KG < 64, "LDS, and what the wait can count");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kLds];
@@ -349,21 +342,8 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
     const uint32_t sw = (uint32_t)(((lane >> 5) ^ ((frow >> 1) & 7)) << 4);
     const uint32_t fw = lds0 + kg * kPart + (uint32_t)(wn * FN * 32 + frow) * 128 + sw;
     const uint32_t fx = lds0 + kg * kPart + (uint32_t)(TN + wm * FM * 32 + frow) * 128 + sw;
-    // what a thread finishes: always the same eight columns, of rows 256 / kAcross apart
-    constexpr int kAcross = TN / 8, kUnits = TM * kAcross > 256 ? TM * kAcross / 256 : 1, kAhead = kUnits < 2 ? 1 : 2;
-    Unit<OutT> unit[kAhead];
-    f32x4 bias[2] = {};
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        const int r = u * (256 / kAcross) + tid / kAcross;
-        unit[u].row = r < TM ? m0 + r : a.rows;
-        unit[u].col = n0 + tid % kAcross * 8;
-        unit[u].first(a);
-    }
-    if (unit[0].col < a.n) {
-        bias[0] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col);
-        bias[1] = *reinterpret_cast<const f32x4 *>(a.bias + unit[0].col + 4);
-    }
+    TileEnd<OutT, TM, TN, KG> end;
+    end.first(a, m0, n0);
     for (int s = 0; s < RING - 1 && s < steps; ++s) request(s);
     for (int s = 0, slot_of = 0; s < steps; ++s, slot_of = slot_of == RING - 1 ? 0 : slot_of + 1) {
         // step s has landed; up to RING - 2 more stay on their way
@@ -396,8 +376,7 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
             if (RING > 2 && h == 0 && more) request(s + RING - 1);
         }
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) unit[u].second(a);
+    end.second(a);
     __syncthreads();                                                  // the ring gives way to the sums
     float *const sums = reinterpret_cast<float *>(smem);
 #pragma unroll
@@ -406,35 +385,11 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4 *>(sums + (kg * TM + (wm * FM + i) * 32 + (lane & 31)) * kStride + (wn * FN + j) * 32 + 8 * q +
+                *reinterpret_cast<f32x4 *>(sums + (kg * TM + (wm * FM + i) * 32 + (lane & 31)) * end.kStride + (wn * FN + j) * 32 + 8 * q +
                                            4 * (lane >> 5)) =
                     f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     __syncthreads();
-    for (int u0 = 0; u0 < kUnits; u0 += kAhead) {
-        if (u0 > 0) {
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                unit[u].row += kAhead * (256 / kAcross);
-                unit[u].first(a);
-            }
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) unit[u].second(a);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int r = (u0 + u) * (256 / kAcross) + tid / kAcross;
-            if (TM * kAcross < 256 && r >= TM) continue;
-            float z[8];
-#pragma unroll
-            for (int g = 0; g < KG; ++g) {
-                const float *const at = sums + (g * TM + r) * kStride + tid % kAcross * 8;
-                const f32x4 lo = *reinterpret_cast<const f32x4 *>(at), hi = *reinterpret_cast<const f32x4 *>(at + 4);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = (g == 0 ? 0.f : z[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]);
-            }
-            unit[u].finish(a, bias, z);
-        }
-    }
+    end.finish(a, sums);
 }
 
 // ---------------------------------------------------------------- few rows (bf16)
@@ -1085,6 +1040,109 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
 #undef AS_SLICE
 }
 
+// ---------------------------------------------------------------- fp32
+
+// A block, four waves as WM x WN x KG (KG shares of the sum, as above), takes TM x TN outputs, KS k of each share at a time:
+// v_mfma_f32_16x16x4_f32, W first (lane l has k = l / 16 of row l % 16 of either operand, and of the result row l % 16, columns
+// 4 (l / 16) .. + 3).  Which k are a lane's first to fourth of sixteen does not matter as long as both operands agree, so a
+// lane takes four in a row with one read, of LDS rows 16 bytes longer than they need be (no two lanes of 16 on one bank).
+// Rows of x and W may start anywhere: 16 bytes at a time through registers, the next step's while this one is worked on.
+template <int WM, int WN, int KG, int FM, int FN, int KS>
+__global__ __launch_bounds__(256) void linear_f32(LinearArgs a, uint32_t mtiles, uint32_t ntiles)
+{
+    static_assert(WM * WN * KG == 4 && KS % 16 == 0, "four waves, whole groups of 16 k");
+    constexpr int TM = WM * FM * 16, TN = WN * FN * 16, kRows = TM + TN, kStep = KG * KS;
+    constexpr int kRow = kStep + 4;                                   // floats of an LDS row
+    constexpr int kMine = kRows * kStep / 4 / 256;                    // pieces of four k that a thread moves
+    static_assert(kRows * kStep % 1024 == 0, "the same for all threads");
+    typedef TileEnd<float, TM, TN, KG> End;
+    constexpr int kLds = 2 * kRows * kRow * 4 > End::kBytes ? 2 * kRows * kRow * 4 : End::kBytes;
+    static_assert(kLds <= 160 * 1024, "LDS");
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kLds];
+    float *const lds = reinterpret_cast<float *>(smem);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
+    const uint32_t bid = blockIdx.x, eight = bid / (8 * mtiles), in = bid % (8 * mtiles);
+    const uint32_t across = ntiles - eight * 8 < 8 ? ntiles - eight * 8 : 8;
+    const int32_t n0 = (int32_t)((eight * 8 + in % across) * TN);
+    const int64_t m0 = (int64_t)(in / across) * TM;
+
+    const float *from[kMine];                                         // rows past either end repeat the last
+    int k_of[kMine], at[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int u = tid + i * 256, r = u / (kStep / 4);
+        k_of[i] = u % (kStep / 4) * 4;
+        at[i] = r * kRow + k_of[i];
+        if (r < TN) {
+            const int32_t n = n0 + r < a.n ? n0 + r : a.n - 1;
+            from[i] = (const float *)a.W + (int64_t)n * a.ldw;
+        } else {
+            const int64_t m = m0 + r - TN < a.rows ? m0 + r - TN : a.rows - 1;
+            from[i] = (const float *)a.x + m * a.ldx;
+        }
+    }
+    f32x4 next[kMine];
+    auto request = [&](int k0) __attribute__((always_inline)) {
+        if (k0 + kStep <= a.k) {                                      // (the same for all)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) next[i] = *reinterpret_cast<const f32x4_any *>(from[i] + k0 + k_of[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = k0 + k_of[i] + e;
+                    const float v = from[i][k < a.k ? k : a.k - 1];
+                    next[i][e] = k < a.k ? v : 0.f;
+                }
+        }
+    };
+    TileEnd<float, TM, TN, KG> end;
+    request(0);
+    end.first(a, m0, n0);
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int fw = (wn * FN * 16 + (lane & 15)) * kRow + kg * KS + (lane >> 4) * 4;
+    const int fx = (TN + wm * FM * 16 + (lane & 15)) * kRow + kg * KS + (lane >> 4) * 4;
+    int slot = 0;
+    for (int k0 = 0; k0 < a.k; k0 += kStep, slot ^= 1) {
+        float *const here = lds + slot * kRows * kRow;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<f32x4 *>(here + at[i]) = next[i];
+        if (k0 + kStep < a.k) request(k0 + kStep);
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < KS / 16; ++g) {
+            f32x4 w[FN], x[FM];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) w[j] = *reinterpret_cast<const f32x4 *>(here + fw + j * 16 * kRow + g * 16);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) x[i] = *reinterpret_cast<const f32x4 *>(here + fx + i * 16 * kRow + g * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[j][e], x[i][e], acc[i][j], 0, 0, 0);
+        }
+    }
+    end.second(a);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            *reinterpret_cast<f32x4 *>(lds + (kg * TM + (wm * FM + i) * 16 + (lane & 15)) * End::kStride + (wn * FN + j) * 16 + 4 * (lane >> 4)) =
+                acc[i][j];
+    __syncthreads();
+    end.finish(a, lds);
+}
+
 // ---------------------------------------------------------------- layer
 
 // The layer's bias in fp32, zeros behind it up to a whole number of 256 columns (and everywhere, where it has none); and the
@@ -1233,13 +1291,49 @@ template <class OutT> static as_status launch_bf16(as_ctx *ctx, const LinearArgs
     }
 }
 
+template <int WM, int WN, int KG, int FM, int FN, int KS> static as_status launch_f32_tile(as_ctx *ctx, const LinearArgs &a)
+{
+    constexpr int TM = WM * FM * 16, TN = WN * FN * 16;
+    const int64_t mtiles = (a.rows + TM - 1) / TM, ntiles = (a.n + TN - 1) / TN;
+    if (mtiles * ntiles > 0x7fffffffLL || mtiles > 0x0fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "product too large for one launch");
+    launch(ctx, kKernelLogits, linear_f32<WM, WN, KG, FM, FN, KS>, dim3((unsigned)(mtiles * ntiles)), dim3(256), 0, a, (uint32_t)mtiles,
+           (uint32_t)ntiles);
+    return AS_OK;
+}
+
+// The same for fp32, by lines fitted to these (us, S stages of 64 k, tiles of 16 x 16 / 16 x 32 / 32 x 64 / 64 x 64 / 128 x 128): 1 x 515 x
+// 1031 4.5 / 5.4 / 9.7 / 14.4 / 40.0; 16 x 512 x 2048 3.8 / 4.6 / 8.8 / 13.3 / 38.6; 16 x 55 x 32128 9.3 / 6.5 / 5.8 / 7.1 / 9.7; 128 x 2048 x
+// 512 8.9 / 13.6 / 28.5 / 46.0 / 146; 333 x 515 x 1031 12.3 / 9.8 / 10.6 / 16.2 / 49.5; 512 x 512 x 2048 - / 18.1 / 15.2 / 15.2 / 42.3; 1024 x
+// 512 x 2048 - / 31.6 / 25.9 / 25.0 / 42.8; 2048 x 1024 x 2048 - / 111 / 89.9 / 82.3 / 80.3; 4000 x 40 x 6000 - / 117 / 59.7 / 56.4 / 50.6.
+static as_status launch_fp32(as_ctx *ctx, const LinearArgs &a)
+{
+    const double S = (double)a.k / kStageK, cus = ctx->num_cus > 0 ? ctx->num_cus : 1;
+    auto units = [&](int64_t tm, int64_t tn) { return ceil((double)((a.rows + tm - 1) / tm) * (double)((a.n + tn - 1) / tn) / cus); };
+    const double t[] = {
+        2.4 + 0.19 * S + (units(16, 16) - 1) * (0.9 + 0.09 * S),
+        2.6 + 0.36 * S + (units(16, 32) - 1) * (0.3 + 0.19 * S),
+        3.2 + 0.78 * S + (units(32, 64) - 1) * (0.3 + 0.66 * S),
+        3.2 + 1.35 * S + (units(64, 64) - 1) * (0.3 + 1.2 * S),
+        4.0 + units(128, 128) * (5.0 + 4.5 * S),
+    };
+    int best = 0;
+    for (int f = 1; f < 5; ++f)
+        if (t[f] < t[best]) best = f;
+    if (ctx->linear_shape > 0 && ctx->linear_shape <= 5) best = ctx->linear_shape - 1;
+    switch (best) {
+    case 0: return launch_f32_tile<1, 1, 4, 1, 1, 32>(ctx, a);
+    case 1: return launch_f32_tile<1, 1, 4, 1, 2, 16>(ctx, a);
+    case 2: return launch_f32_tile<1, 2, 2, 2, 2, 16>(ctx, a);
+    case 3: return launch_f32_tile<2, 2, 1, 2, 2, 32>(ctx, a);
+    default: return launch_f32_tile<2, 2, 1, 4, 4, 16>(ctx, a);
+    }
+}
+
 as_status launch_linear(as_ctx *ctx, const as_layer *l, LinearArgs a)
 {
     as_status st = AS_OK;
     if (l->wdtype == AS_F32) {
-        const int64_t mtiles = (a.rows + 63) / 64, blocks = mtiles * ((a.n + 63) / 64);
-        if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "product too large for one launch");
-        launch(ctx, kKernelLogits, linear_any<float, float>, dim3((unsigned)blocks), dim3(256), 0, a, (int32_t)mtiles);
+        st = launch_fp32(ctx, a);
     } else {
         if (!x_as_it_is(l, a.x, a.ldx)) {
             const int64_t blocks = (a.rows * l->kp + 255) / 256;

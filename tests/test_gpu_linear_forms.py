@@ -69,3 +69,22 @@ def test_rows_of_weights_and_x_apart(form):
     for pad, wpad in ((8, 16), (3, 0), (0, 5)):
         B.as_linear(context(rows, form), B.Layer(apart(W, wpad), bias=b), apart(x, pad), out)
         check(out, x, W, b, "none", 1.0, None, (form, pad, wpad))
+
+
+@pytest.mark.parametrize("form", range(1, 6))
+@pytest.mark.parametrize("rows,k,n", [(1, 1, 1), (3, 7, 33), (17, 130, 130), (70, 515, 300), (300, 64, 1031)])
+def test_fp32(form, rows, k, n):
+    x, W, b, r = problem(rows, k, n, torch.float32, torch.float32, seed=form + n, residual=True)
+    p = inputs(rows, n, seed=n, L=20)
+    out = torch.full((rows, n + 3), 77.0, device="cuda")
+    for xpad, wpad, opad in ((0, 0, 0), (3, 5, 1)):
+        B.as_linear(context(rows, form), B.Layer(apart(W, wpad), bias=b, act="silu"), apart(x, xpad), out[:, :n], residual=apart(r, opad))
+        check(out[:, :n], x, W, b, "silu", 1.0, r, (form, rows, k, n))
+    B.as_linear(context(rows, form), B.Layer(W), x, out[:, :n], shaping=to_shaping(p, rows, n, ALL))
+    z = x.double().cpu() @ W.double().cpu().t()
+    q = ((x.double().cpu() ** 2) @ (W.double().cpu().t() ** 2)).sqrt()
+    extra = (8 * 1.13 * k ** 0.5 * 2.0 ** -23 * q + 2.0 ** -18 * z.abs() + 2.0 ** -22 * z.abs()).numpy()
+    extra = extra * np.maximum(p["repetition"], 1 / p["repetition"]).astype(np.float64)[:, None]
+    want, size = shaped64(z.numpy(), p, ALL)
+    compare(out[:, :n], want, size, torch.float32, (form, rows, k, n), extra)
+    assert bool((out[:, n:] == 77.0).all()), "wrote outside its columns"
