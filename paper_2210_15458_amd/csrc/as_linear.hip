@@ -485,245 +485,9 @@ template <int OFFSET> __device__ __forceinline__ bf16x8 lds_read8(uint32_t at)
     return r;
 }
 
-// A wave's 64 x 128 outputs shaped.  What the rows say of them (strengths, table rows, bits) is requested into the wave's LDS while
-// the products run, one word of each row a lane, and taken from there when the sums are done.  The seen columns, few as a rule
-// and anywhere, are then listed in that LDS and dealt out, kDealt a lane, so that their counts come in one go; each lane
-// puts its penalties on the sums where they lie turned in LDS (32 x 32 of them at a time), and biases and masks follow,
-// eight columns a lane.  Where more are seen (the first columns of a vocabulary ordered by frequency) the counts of all
-// columns are read, eight a lane: as many bytes as that many lines.
-constexpr int kDealt = 2;                     // seen columns of 32 x 128, a lane
-constexpr uint32_t kOfRows = 512, kOfBits = kOfRows + 5 * 256;       // in the wave's LDS, behind the bias
-
-// Requests of a tile's rows m .. m + 63 and columns n .. n + 127.
-__device__ __forceinline__ void request_rows(const LinearArgs &a, unsigned char *stage, int64_t m, int32_t n, int lane)
-{
-    const as_shaping &s = a.shape;
-    const int64_t row = m + lane < a.rows ? m + lane : a.rows - 1;
-    auto word = [&](const void *p, uint32_t at) __attribute__((always_inline)) {
-        __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(stage + at), 4, 0, 0);
-    };
-    if (s.repetition) word(s.repetition + row, kOfRows);
-    if (s.presence) word(s.presence + row, kOfRows + 256);
-    if (s.frequency) word(s.frequency + row, kOfRows + 512);
-    if (s.bias_ids) word(s.bias_ids + row, kOfRows + 768);
-    if (s.mask_ids) word(s.mask_ids + row, kOfRows + 1024);
-    if (s.seen) {
-        const int32_t words = (a.n + 31) >> 5;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int32_t w = (n >> 5) + e < words ? (n >> 5) + e : words - 1;
-            word(s.seen + row * s.seen_ld + w, kOfBits + e * 256);
-        }
-    }
-}
-
-// What a lane (row b of either 32, half h of the columns) has of that.
-struct ShapeTile {
-    float repetition[2], inverse[2], presence[2], frequency[2];
-    int32_t bias[2];                          // the row of the table, -1: none, -2: the row is not to be written
-    uint32_t seen[2][2], mask[2][2];          // words 2h and 2h + 1
-    int total[2];                             // seen columns of the wave's 32 rows; if dealt out:
-    int32_t place[2][kDealt];                 // row * 128 + column, or -1
-    float less[2][kDealt];                    // what it is to lose
-};
-
-__device__ __forceinline__ uint32_t lds_word(uint32_t at)
-{
-    uint32_t v;
-    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ float lds_float(uint32_t at) { return __builtin_bit_cast(float, lds_word(at)); }
-__device__ __forceinline__ int32_t table_row(int64_t id, int64_t rows) { return (int32_t)(id < rows ? id : rows - 1); }
-
-__device__ __forceinline__ void take_rows(const LinearArgs &a, ShapeTile &t, uint32_t stage, int64_t m, int32_t n, int lane)
-{
-    const as_shaping &s = a.shape;
-    const int b = lane & 31, h = lane >> 5;
-    const int32_t words = (a.n + 31) >> 5;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t row = m + i * 32 + b, last = a.rows - 1, mine = row < last ? row : last;
-        const uint32_t at = stage + (uint32_t)(i * 32 + b) * 4;
-        t.repetition[i] = s.repetition ? lds_float(at + kOfRows) : 1.f;
-        t.presence[i] = s.presence ? lds_float(at + kOfRows + 256) : 0.f;
-        t.frequency[i] = s.frequency ? lds_float(at + kOfRows + 512) : 0.f;
-        t.inverse[i] = 1.f / t.repetition[i];
-        t.bias[i] = -1;
-        if (s.bias) {
-            t.bias[i] = table_row(s.bias_ids ? (int32_t)lds_word(at + kOfRows + 768) : s.bias_rows == 1 ? 0 : mine, s.bias_rows);
-            t.bias[i] = t.bias[i] < 0 ? -1 : t.bias[i];
-        }
-        const bool done = row > last || (s.finished && s.finished[mine]);
-        if (done) t.bias[i] = -2;
-        int32_t id = -1;
-        if (s.mask) id = table_row(s.mask_ids ? (int32_t)lds_word(at + kOfRows + 1024) : s.mask_rows == 1 ? 0 : mine, s.mask_rows);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int32_t word = (n >> 5) + 2 * h + e, left = a.n - word * 32;
-            t.mask[i][e] = id < 0 ? 0xffffffffu : s.mask[id * s.mask_ld + (word < words ? word : words - 1)];
-            t.seen[i][e] = s.seen && !done ? lds_word(at + kOfBits + (2 * h + e) * 256) : 0u;
-            if (left < 32) t.seen[i][e] &= left > 0 ? (1u << left) - 1u : 0u;
-        }
-    }
-    if (!s.seen) return;
-    int32_t count[2][kDealt];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int mine = __popc(t.seen[i][0]) + __popc(t.seen[i][1]);
-        const int upto = (int)wave_scan_add((float)mine);
-        t.total[i] = __builtin_amdgcn_readlane(upto, 63);
-        if (t.total[i] > kDealt * kWave) continue;
-        uint32_t at = stage + i * 1024 + (uint32_t)(upto - mine) * 4;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            for (uint32_t w = t.seen[i][e]; w; w &= w - 1, at += 4)
-                asm volatile("ds_write_b32 %0, %1" ::"v"(at), "v"(b * 128 + (2 * h + e) * 32 + __ffs((int)w) - 1) : "memory");
-#pragma unroll
-        for (int k = 0; k < kDealt; ++k) {
-            t.place[i][k] = -1;
-            count[i][k] = 0;
-            if (k * kWave >= t.total[i]) continue;                    // (the same for the whole wave)
-            const int32_t p = (int32_t)lds_word(stage + i * 1024 + (uint32_t)(k * kWave + lane) * 4);
-            if (k * kWave + lane < t.total[i]) t.place[i][k] = p;
-            if (s.counts && t.place[i][k] >= 0)
-                count[i][k] = s.counts[(m + i * 32 + (p >> 7)) * s.counts_ld + n + (p & 127)];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int k = 0; k < kDealt; ++k) {
-            if (t.total[i] > kDealt * kWave || k * kWave >= t.total[i]) continue;
-            const int from = t.place[i][k] >= 0 ? t.place[i][k] >> 7 : 0;
-            ShapeRow of;
-            of.frequency = __shfl(t.frequency[i], from, kWave);
-            of.presence = __shfl(t.presence[i], from, kWave);
-            t.less[i][k] = lost(of, count[i][k]);
-        }
-}
-
-// The half of it that is rows m .. m + 31, sums `acc` (lane b + 32 h has row b), to memory.
-template <class OutT, int I>
-__device__ __forceinline__ void shape_sums(const LinearArgs &a, const ShapeTile &t, f32x16 (&acc)[4], uint32_t stage, int64_t m, int32_t n, int lane)
-{
-    const as_shaping &s = a.shape;
-    const int b = lane & 31, h = lane >> 5;
-    const bool dealt = t.total[I] <= kDealt * kWave;
-    // where the lane's eight columns of the turned sums come from: row lane / 4 and the one 16 on
-    const int row = lane >> 2, c = (lane & 3) * 2;
-    int32_t bias[2];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) bias[p] = __shfl(t.bias[I], p * 16 + row, kWave);
-    f32x4 add[2][2];
-    i32x4_any count[2][2];
-    // what the lane needs of its columns of 32 x 32 number j
-    auto ahead = [&](int j) __attribute__((always_inline)) {
-        const int32_t col = n + j * 32 + c * 4;
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            if (s.bias) {
-                add[p][0] = add[p][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-                const float *const from = s.bias + bias[p] * s.bias_ld + col;
-                if (bias[p] >= 0 && col + 8 <= a.n) {
-                    add[p][0] = *reinterpret_cast<const f32x4_any *>(from);
-                    add[p][1] = *reinterpret_cast<const f32x4_any *>(from + 4);
-                } else if (bias[p] >= 0) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < a.n) add[p][e >> 2][e & 3] = from[e];
-                }
-            }
-            if (s.counts && !dealt) {
-                const int32_t *const from = s.counts + (m + p * 16 + row) * s.counts_ld + col;
-                if (bias[p] != -2 && col + 8 <= a.n) {
-                    count[p][0] = *reinterpret_cast<const i32x4_any *>(from);
-                    count[p][1] = *reinterpret_cast<const i32x4_any *>(from + 4);
-                } else if (bias[p] != -2) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < a.n) count[p][e >> 2][e & 3] = from[e];
-                }
-            }
-        }
-    };
-    ahead(0);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 w = {acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
-            asm volatile("ds_write_b128 %0, %1" ::"v"(stage + b * 128 + (((q * 2 + h) ^ (b & 7)) << 4)), "v"(w) : "memory");
-        }
-        if (s.seen && dealt) {
-#pragma unroll
-            for (int k = 0; k < kDealt; ++k) {
-                if (k * kWave >= t.total[I]) continue;
-                const int32_t place = t.place[I][k];
-                const int pr = place >= 0 ? place >> 7 : 0, pc = place & 31;
-                const float up = __shfl(t.inverse[I], pr, kWave), down = __shfl(t.repetition[I], pr, kWave);
-                if (place < 0 || (place & 127) >> 5 != j) continue;
-                const uint32_t at = stage + pr * 128 + (((pc >> 2) ^ (pr & 7)) << 4) + (pc & 3) * 4;
-                float y = lds_float(at);
-                y = fmaf(y, y > 0.f ? up : down, -t.less[I][k]);
-                asm volatile("ds_write_b32 %0, %1" ::"v"(at), "v"(y) : "memory");
-            }
-        }
-        f32x4 v[4];
-        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
-                     "s_waitcnt lgkmcnt(0)"
-                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-                     : "v"(stage + row * 128 + ((c ^ (row & 7)) << 4)), "v"(stage + row * 128 + (((c + 1) ^ (row & 7)) << 4))
-                     : "memory");
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const int from = p * 16 + row, word = from + 32 * (j >> 1);
-            if (s.seen && !dealt) {
-                const uint32_t bits = (uint32_t)__shfl((int)t.seen[I][j & 1], word, kWave) >> ((lane & 3) * 8);
-                ShapeRow of;
-                of.frequency = __shfl(t.frequency[I], from, kWave);
-                of.presence = __shfl(t.presence[I], from, kWave);
-                of.inverse = __shfl(t.inverse[I], from, kWave);
-                of.repetition = __shfl(t.repetition[I], from, kWave);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float y = v[2 * p + (e >> 2)][e & 3];
-                    v[2 * p + (e >> 2)][e & 3] = shape1(of, bits >> e & 1u, s.counts ? count[p][e >> 2][e & 3] : 0, 0.f, true, y);
-                }
-            }
-            if (s.bias) {
-                v[2 * p] += add[p][0];
-                v[2 * p + 1] += add[p][1];
-            }
-            if (s.mask) {
-                const uint32_t free = (uint32_t)__shfl((int)t.mask[I][j & 1], word, kWave) >> ((lane & 3) * 8);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[2 * p + (e >> 2)][e & 3] = free >> e & 1u ? v[2 * p + (e >> 2)][e & 3] : -__builtin_inff();
-            }
-        }
-        if (j < 3) ahead(j + 1);
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            float z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = v[2 * p + (e >> 2)][e & 3];
-            const int32_t col = n + j * 32 + c * 4, left = a.n - col;
-            if (bias[p] == -2 || left <= 0) continue;
-            OutT *const to = (OutT *)a.out + (m + p * 16 + row) * a.ldo + col;
-            if (left >= 8) {
-                store8(to, z);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (e < left) store1(to + e, z[e]);
-            }
-        }
-    }
-}
-
 // The epilogue of a wave's 64 x 128: bias and activation where the sums are, then turned through the wave's own 4 KB of LDS, so
-// that a lane holds eight consecutive columns of a row.  With nothing further to do bf16 outputs are turned as such, 32 x 64
-// at a time, and written in whole lines; fp32 outputs, and those that have a residual or a shaping before they are rounded,
+// that a lane holds eight consecutive columns of a row.  With no residual bf16 outputs are turned as such, 32 x 64
+// at a time, and written in whole lines; fp32 outputs, and those that have a residual before they are rounded,
 // 32 x 32 at a time.  16-byte piece c of the 128 bytes of LDS row r lies at c ^ (r & 7).  The LDS accesses are written by hand, so
 // that the compiler does not tie them to the requests in flight.
 template <class OutT, int FORM>
@@ -746,8 +510,6 @@ __device__ __forceinline__ int big_epilogue(const LinearArgs &a, f32x16 (&acc)[2
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = fmaf(acc[i][j][4 * q + e], a.scale, add[q][e]);
     }
-    [[maybe_unused]] ShapeTile tile;         // (its loads are on their way while the activation is worked out)
-    if constexpr (FORM == 2) take_rows(a, tile, stage, m, n, lane);
     if (a.act != AS_ACT_NONE) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -807,11 +569,6 @@ __device__ __forceinline__ int big_epilogue(const LinearArgs &a, f32x16 (&acc)[2
                 }
             }
         return inside ? 16 : -1;
-    } else if constexpr (FORM == 2) {
-        shape_sums<OutT, 0>(a, tile, acc[0], stage, m, n, lane);
-        shape_sums<OutT, 1>(a, tile, acc[1], stage, m + 32, n, lane);
-        // (loads that were waited for meanwhile only leave less behind)
-        return inside && __all(tile.bias[0] != -2 && tile.bias[1] != -2) ? 8 * (int)sizeof(OutT) : -1;
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -842,6 +599,335 @@ __device__ __forceinline__ int big_epilogue(const LinearArgs &a, f32x16 (&acc)[2
             }
         return FORM == 0 && inside ? 32 : -1;
     }
+}
+
+// The epilogue of a wave's 64 x 128 with a shaping.  The sums stay where they are: lane b + 32 h of a 32 x 32 holds row b, columns 8 q + 4 h .. + 3,
+// q = 0..3, and everything up to the rounding is done there.  Then lanes exchange halves (v_permlane32_swap, v_permlane16_swap),
+// after which a store instruction writes 16 rows of 64 bytes: lane l has row 16 t + l % 16 of store t, and 16 bytes 16 u + 8 h (bf16)
+// columns on, u = l / 16 % 2.  No LDS, no waiting.
+constexpr uint32_t kOfRows = 512, kOfBits = kOfRows + 5 * 256;       // in the wave's LDS, behind the bias
+constexpr uint32_t kOfList = kOfBits + 4 * 256;                       // behind those what seen columns lose, as many as there is room for
+constexpr int kListedBig = (kBigStage - (int)kOfList) / 4;
+
+__device__ __forceinline__ uint32_t lds_word(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds_float(uint32_t at) { return __builtin_bit_cast(float, lds_word(at)); }
+__device__ __forceinline__ void swap32(uint32_t &x, uint32_t &y)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = r[0];
+    y = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t &x, uint32_t &y)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = r[0];
+    y = r[1];
+}
+// 32 x 32 outputs between the lanes that have the sums and those that meet memory; word w of store t.
+struct Turned {
+    uint32_t v[2][4];
+};
+__device__ __forceinline__ void turn(Turned &t)                       // bf16: v[q % 2][...] from [q][word]
+{
+    // t.v[s][0..1] are quad 2 s, t.v[s][2..3] quad 2 s + 1
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) swap32(t.v[s][w], t.v[s][2 + w]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) swap16(t.v[0][w], t.v[1][w]);
+}
+// Requests of what the rows say of a tile's rows m .. m + 63 and columns n .. n + 127, into the wave's LDS, a word of each row a lane.
+__device__ __forceinline__ void request_rows(const LinearArgs &a, unsigned char *stage, int64_t m, int32_t n, int lane)
+{
+    const as_shaping &s = a.shape;
+    const int64_t row = m + lane < a.rows ? m + lane : a.rows - 1;
+    auto word = [&](const void *p, uint32_t at) __attribute__((always_inline)) {
+        __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(stage + at), 4, 0, 0);
+    };
+    if (s.repetition) word(s.repetition + row, kOfRows);
+    if (s.presence) word(s.presence + row, kOfRows + 256);
+    if (s.frequency) word(s.frequency + row, kOfRows + 512);
+    if (s.bias_ids) word(s.bias_ids + row, kOfRows + 768);
+    if (s.mask_ids) word(s.mask_ids + row, kOfRows + 1024);
+    if (s.seen) {
+        const int32_t words = (a.n + 31) >> 5;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int32_t w = (n >> 5) + e < words ? (n >> 5) + e : words - 1;
+            word(s.seen + row * s.seen_ld + w, kOfBits + e * 256);
+        }
+    }
+}
+
+// What a lane has of that, of row b of 32.
+struct ShapeTile {
+    float repetition, inverse, presence, frequency;
+    const float *bias;                        // the row's in the table, from column n on, or null
+    bool done;                                // the row is not to be written
+    uint32_t seen[4];                         // the bits of its own columns
+};
+__device__ __forceinline__ int64_t table_row(int64_t id, int64_t rows) { return id < rows ? id : rows - 1; }
+
+// The words of the row's mask.
+__device__ __forceinline__ void mask_words(const LinearArgs &a, uint32_t stage, int64_t m, int32_t n, int i, int lane, uint32_t (&mask)[4])
+{
+    const as_shaping &s = a.shape;
+    const int b = lane & 31;
+    const int32_t words = (a.n + 31) >> 5;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mask[e] = 0xffffffffu;
+    if (!s.mask) return;
+    const int64_t row = m + i * 32 + b, last = a.rows - 1, mine = row < last ? row : last;
+    const int64_t id = table_row(s.mask_ids ? (int32_t)lds_word(stage + kOfRows + 1024 + (uint32_t)(i * 32 + b) * 4) : s.mask_rows == 1 ? 0 : mine, s.mask_rows);
+    if (id < 0) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mask[e] = s.mask[id * s.mask_ld + ((n >> 5) + e < words ? (n >> 5) + e : words - 1)];
+}
+
+__device__ __forceinline__ void take_rows(const LinearArgs &a, ShapeTile &t, uint32_t stage, int64_t m, int32_t n, int i, int lane)
+{
+    const as_shaping &s = a.shape;
+    const int b = lane & 31, h = lane >> 5;
+    const int64_t row = m + i * 32 + b, last = a.rows - 1, mine = row < last ? row : last;
+    const uint32_t at = stage + (uint32_t)(i * 32 + b) * 4;
+    t.repetition = s.repetition ? lds_float(at + kOfRows) : 1.f;
+    t.presence = s.presence ? lds_float(at + kOfRows + 256) : 0.f;
+    t.frequency = s.frequency ? lds_float(at + kOfRows + 512) : 0.f;
+    t.inverse = 1.f / t.repetition;
+    t.bias = nullptr;
+    if (s.bias) {
+        const int64_t id = table_row(s.bias_ids ? (int32_t)lds_word(at + kOfRows + 768) : s.bias_rows == 1 ? 0 : mine, s.bias_rows);
+        if (id >= 0) t.bias = s.bias + id * s.bias_ld + n;
+    }
+    t.done = row > last || (s.finished && s.finished[mine]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t left = a.n - n - e * 32;
+        t.seen[e] = s.seen && !t.done ? lds_word(at + kOfBits + e * 256) & (0x0f0f0f0fu << 4 * h) : 0u;
+        if (left < 32) t.seen[e] &= left > 0 ? (1u << left) - 1u : 0u;
+    }
+}
+
+// The seen columns of 32 rows from m on, few as a rule and anywhere, listed in the wave's LDS, their counts fetched by the list, all at
+// once, and what each is to lose left in its place; a lane's own, `at` on, in the order in which it comes to them.  False where the
+// list is too short for them (the first columns of a vocabulary ordered by frequency): then a lane reads the counts of all its columns.
+__device__ __forceinline__ bool list_losses(const LinearArgs &a, const ShapeTile &t, uint32_t list, int64_t m, int32_t n, int lane, int &at)
+{
+    const as_shaping &s = a.shape;
+    const int mine = __popc(t.seen[0]) + __popc(t.seen[1]) + __popc(t.seen[2]) + __popc(t.seen[3]);
+    const int upto = (int)wave_scan_add((float)mine);
+    const int total = __builtin_amdgcn_readlane(upto, 63);
+    at = upto - mine;
+    if (total > kListedBig) return false;
+    uint32_t put = list + (uint32_t)at * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        for (uint32_t w = t.seen[e]; w; w &= w - 1, put += 4)
+            asm volatile("ds_write_b32 %0, %1" ::"v"(put), "v"((lane & 31) * 128 + e * 32 + __ffs((int)w) - 1) : "memory");
+    for (int k0 = 0; k0 < total; k0 += 2 * kWave) {                   // (the same for the whole wave)
+        int32_t place[2], count[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = k0 + k * kWave + lane;
+            place[k] = i < total ? (int32_t)lds_word(list + (uint32_t)i * 4) : 0;
+            count[k] = 0;
+            if (i < total) count[k] = s.counts[(m + (place[k] >> 7)) * s.counts_ld + n + (place[k] & 127)];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = k0 + k * kWave + lane;
+            ShapeRow of;
+            of.frequency = __shfl(t.frequency, place[k] >> 7, kWave);
+            of.presence = __shfl(t.presence, place[k] >> 7, kWave);
+            const float less = lost(of, count[k]);
+            if (i < total) asm volatile("ds_write_b32 %0, %1" ::"v"(list + (uint32_t)i * 4), "v"(less) : "memory");
+        }
+    }
+    return true;
+}
+
+// Gives the number of stores that it has requested last, where that is the same for all lanes, or -1.
+// The 32 x 32s go through one piece of code in turn, which is fetched once: unrolled, the epilogue is some 10000 instructions that
+// a compute unit comes by twice in a launch, and the first time waits for each line of them.
+template <class OutT>
+__device__ __forceinline__ int shaped_epilogue(const LinearArgs &a, f32x16 (&acc)[2][4], uint32_t stage, int64_t m, int32_t n, int lane)
+{
+    asm volatile("" : "+v"(lane));           // (its addresses are worked out here: kept over the products they would not fit)
+    const as_shaping &s = a.shape;
+    const int b = lane & 31, h = lane >> 5;
+    uint32_t masks[2][4];
+    mask_words(a, stage, m, n, 0, lane, masks[0]);
+    mask_words(a, stage, m, n, 1, lane, masks[1]);
+    // a lane's place in the stores: row 16 t + lane % 16, columns from `first` on
+    const int u = lane >> 4 & 1, first = sizeof(OutT) == 2 ? 16 * u + 8 * h : 8 * u + 4 * h;
+    constexpr int kEach = 16 / (int)sizeof(OutT);                     // columns of a lane's 16 bytes
+    bool whole = m + 64 <= a.rows && n + 128 <= a.n;
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i, m += 32) {
+        ShapeTile tile;
+        uint64_t skip = 0;
+        int at = 0;
+        bool listed = true;
+        f32x4 more[4];
+        auto biases = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t c = j * 32 + 8 * q + 4 * h;
+                more[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (tile.bias == nullptr) continue;
+                if (n + c + 4 <= a.n) {
+                    more[q] = *reinterpret_cast<const f32x4_any *>(tile.bias + c);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n + c + e < a.n) more[q][e] = tile.bias[c + e];
+                }
+            }
+        };
+        i32x4_any all[4];
+        auto counts = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t c = n + j * 32 + 8 * q + 4 * h;
+                const int32_t *const from = s.counts + (m + b) * s.counts_ld + c;
+                all[q] = i32x4_any{0, 0, 0, 0};
+                if (tile.done) continue;
+                if (c + 4 <= a.n) {
+                    all[q] = *reinterpret_cast<const i32x4_any *>(from);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < a.n) all[q][e] = from[e];
+                }
+            }
+        };
+        take_rows(a, tile, stage, m - i * 32, n, i, lane);
+        skip = __ballot(tile.done);
+        whole = whole && skip == 0;
+        if (s.bias) biases(0);
+        if (s.counts) listed = list_losses(a, tile, stage + kOfList, m, n, lane, at);
+        if (!listed) counts(0);
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            f32x16 &t = acc[0][0];
+            f32x4 add[4];                    // (the bias lies in the wave's LDS)
+            asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\tds_read_b128 %3, %4 offset:96\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(add[0]), "=&v"(add[1]), "=&v"(add[2]), "=&v"(add[3])
+                         : "v"(stage + j * 128 + h * 16)
+                         : "memory");
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = fmaf(t[e], a.scale, add[e >> 2][e & 3]);
+            activate<OutT, 16>(t, a.act, a.act_arg, a.act_inv);
+            if (s.seen) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t bits = tile.seen[0] >> (8 * q + 4 * h) & 15u;
+                    if (!__any(bits != 0)) continue;
+                    f32x4 less = {0.f, 0.f, 0.f, 0.f};
+                    if (s.counts && listed) {
+                        uint32_t p[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int k = at + __popc(bits & ((1u << e) - 1u));
+                            p[e] = stage + kOfList + (uint32_t)(k < kListedBig ? k : kListedBig - 1) * 4;
+                        }
+                        float l[4];
+                        asm volatile("ds_read_b32 %0, %4\n\tds_read_b32 %1, %5\n\tds_read_b32 %2, %6\n\tds_read_b32 %3, %7\n\t"
+                                     "s_waitcnt lgkmcnt(0)"
+                                     : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3])
+                                     : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3])
+                                     : "memory");
+                        less = f32x4{l[0], l[1], l[2], l[3]};
+                        at += __popc(bits);
+                    } else if (s.counts) {
+                        ShapeRow of;
+                        of.frequency = tile.frequency;
+                        of.presence = tile.presence;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) less[e] = lost(of, all[q][e]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = t[4 * q + e], v = fmaf(y, y > 0.f ? tile.inverse : tile.repetition, -less[e]);
+                        t[4 * q + e] = bits >> e & 1u ? v : y;
+                    }
+                }
+            }
+            if (!listed && j < 3) counts(j + 1);
+            if (s.bias) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) t[e] += more[e >> 2][e & 3];
+                if (j < 3) biases(j + 1);
+            }
+            if (s.mask) {
+                const uint32_t free = masks[0][0] >> 4 * h;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) t[e] = free >> (8 * (e >> 2) + (e & 3)) & 1u ? t[e] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int half = 0; half < (sizeof(OutT) == 2 ? 1 : 2); ++half) {      // fp32: 32 x 16 at a time
+                const int32_t col = n + j * 32 + half * 16 + first, left = a.n - col;
+                Turned w;
+                if constexpr (sizeof(OutT) == 2) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w.v[k >> 2][k & 3] = pack2_bf16(t[2 * k], t[2 * k + 1]);
+                    turn(w);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float y = t[8 * half + e];
+                        w.v[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, y);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) swap16(w.v[0][k], w.v[1][k]);
+                }
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int in = p * 16 + (lane & 15);
+                    const int64_t row = m + in;
+                    OutT *const to = (OutT *)a.out + row * a.ldo + col;
+                    const u32x4_any v = {w.v[p][0], w.v[p][1], w.v[p][2], w.v[p][3]};
+                    if (whole) {
+                        *reinterpret_cast<u32x4_any *>(to) = v;
+                    } else if (row < a.rows && !(skip >> in & 1u)) {
+                        if (left >= kEach) {
+                            *reinterpret_cast<u32x4_any *>(to) = v;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < kEach - 1; ++e)
+                                if (e < left) {
+                                    const uint32_t x = v[sizeof(OutT) == 2 ? e >> 1 : e];
+                                    if constexpr (sizeof(OutT) == 2) to[e] = (OutT)(x >> (e & 1) * 16);
+                                    else to[e] = __builtin_bit_cast(OutT, x);
+                                }
+                        }
+                    }
+                }
+            }
+            // the next 32 x 32 takes this one's place
+#pragma unroll
+            for (int k = 0; k < 3; ++k) acc[0][k] = acc[0][k + 1];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                tile.seen[k] = tile.seen[k + 1];
+                masks[0][k] = masks[0][k + 1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            acc[0][k] = acc[1][k];
+            masks[0][k] = masks[1][k];
+        }
+    }
+    // (loads that were waited for meanwhile only leave less behind)
+    return whole ? 8 * (int)sizeof(OutT) : -1;
 }
 
 // FORM: what follows the activation, 0 nothing, 1 a residual, 2 a shaping.
@@ -1025,7 +1111,9 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
             if (more) requested();
         }
         AS_WAIT(xa, wa);                                              // (in flight they must not meet other code)
-        stores = big_epilogue<OutT, FORM>(a, acc, lds0 + 2 * kBigRing + (uint32_t)wave * kBigStage, m0 + wm * 64, n0 + wn * 128, lane);
+        const uint32_t stage = lds0 + 2 * kBigRing + (uint32_t)wave * kBigStage;
+        if constexpr (FORM == 2) stores = shaped_epilogue<OutT>(a, acc, stage, m0 + wm * 64, n0 + wn * 128, lane);
+        else stores = big_epilogue<OutT, FORM>(a, acc, stage, m0 + wm * 64, n0 + wn * 128, lane);
         // the first fragments of the next tile, again: they do not take the epilogue's registers
         const uint32_t so = (uint32_t)(gs & 1) * kBigRing;
         AS_RX(xa, 0, so, 0); AS_RX(xa, 1, so, 0);
@@ -1152,11 +1240,33 @@ template <class T> __global__ __launch_bounds__(256) void layer_bias_kernel(cons
     const int32_t i = (int32_t)(blockIdx.x * 256 + threadIdx.x);
     if (i < padded) out[i] = bias && i < n ? widen(bias[i]) : 0.f;
 }
-__global__ __launch_bounds__(256) void layout_kernel(const uint16_t *in, int64_t ld, int64_t rows, int32_t k, uint16_t *out, int32_t kp)
+// eight elements a thread, `pieces` of them a row
+__global__ __launch_bounds__(256) void layout_kernel(const uint16_t *in, int64_t ld, int64_t rows, int32_t k, uint16_t *out, uint32_t pieces)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / kp;
-    const int32_t c = (int32_t)(i - row * kp);
-    if (row < rows) out[i] = c < k ? in[row * ld + c] : 0;
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = i >> 32 ? (int64_t)(i / pieces) : (int64_t)((uint32_t)i / pieces);
+    const int32_t c = (int32_t)(i - row * pieces) * 8;
+    if (row >= rows) return;
+    const uint16_t *const from = in + row * ld + c;
+    u32x4_any v = {0, 0, 0, 0};
+    if (c + 8 <= k) {
+        v = fetch16<false>(from);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < k) v[e >> 1] |= (uint32_t)from[e] << (e & 1) * 16;
+    }
+    put16<false>(out + row * (int64_t)pieces * 8 + c, v);
+}
+
+static as_status launch_layout(as_ctx *ctx, hipStream_t stream, const void *in, int64_t ld, int64_t rows, int32_t k, void *out, int32_t kp)
+{
+    const int64_t blocks = (rows * (kp / 8) + 255) / 256;
+    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "too large to lay out");
+    hipLaunchKernelGGL(layout_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, (const uint16_t *)in, ld, rows, k, (uint16_t *)out,
+                       (uint32_t)(kp / 8));
+    AS_HIP_TRY(ctx, hipGetLastError());
+    return AS_OK;
 }
 
 as_status launch_layer_layout(const as_layer &l, const void *W, int64_t ldw, const void *bias)
@@ -1169,11 +1279,8 @@ as_status launch_layer_layout(const as_layer &l, const void *W, int64_t ldw, con
         hipLaunchKernelGGL(layer_bias_kernel<float>, grid, dim3(256), 0, nullptr, (const float *)bias, l.bias, l.n, padded);
     AS_HIP_TRY(nullptr, hipGetLastError());
     if (l.own) {
-        const int64_t blocks = ((int64_t)l.n * l.kp + 255) / 256;
-        if (blocks > 0x7fffffffLL) return fail(nullptr, AS_ERR_UNSUPPORTED, "weights too large to lay out");
-        hipLaunchKernelGGL(layout_kernel, dim3((unsigned)blocks), dim3(256), 0, nullptr, (const uint16_t *)W, ldw, (int64_t)l.n, l.k,
-                           (uint16_t *)l.own, l.kp);
-        AS_HIP_TRY(nullptr, hipGetLastError());
+        const as_status st = launch_layout(nullptr, nullptr, W, ldw, l.n, l.k, l.own, l.kp);
+        if (st != AS_OK) return st;
     }
     AS_HIP_TRY(nullptr, hipStreamSynchronize(nullptr));
     return AS_OK;
@@ -1336,10 +1443,8 @@ as_status launch_linear(as_ctx *ctx, const as_layer *l, LinearArgs a)
         st = launch_fp32(ctx, a);
     } else {
         if (!x_as_it_is(l, a.x, a.ldx)) {
-            const int64_t blocks = (a.rows * l->kp + 255) / 256;
-            if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "x too large to lay out");
-            hipLaunchKernelGGL(layout_kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, (const uint16_t *)a.x, a.ldx, a.rows,
-                               l->k, (uint16_t *)ctx->linear_x.ptr, l->kp);
+            st = launch_layout(ctx, ctx->stream, a.x, a.ldx, a.rows, l->k, ctx->linear_x.ptr, l->kp);
+            if (st != AS_OK) return st;
             a.x = ctx->linear_x.ptr;
             a.ldx = l->kp;
         }
