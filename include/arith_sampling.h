@@ -154,7 +154,7 @@ as_status as_ctx_set_tuning(as_ctx *ctx, as_tuning knob, int32_t value);
  * own start/stop HIP events, taken from the dispatch on the context's stream.
  * as_ctx_profile_read synchronises the stream, returns the summed kernel time
  * and the number of timed launches since the last read for
- *   kernel 0: fused sampling step   1: logits (bigram) kernel   2: threshold   3: interval (encode) step
+ *   kernel 0: fused sampling step   1: logits (bigram) and layers   2: threshold   3: interval (encode) step
  * and resets the counters.  (A decode that makes the logits rows of all tokens before its
  * first step has that launch under 1, what it makes of the rows under 2, and its steps, which
  * share one launch, under 0; one that makes rows for the tokens that come has these a few times
@@ -518,7 +518,8 @@ as_status as_shape_logits(as_ctx *ctx, const void *logits, int64_t rows, int64_t
  * W is borrowed, must outlive the layer and keep its contents where it is fp32
  * or its rows start on 16 bytes and k is a multiple of 64; other bf16 weights
  * are read once here (the layer keeps a copy in rows of that kind).  The call
- * enqueues kernels on the default stream and waits for them.
+ * enqueues kernels on the default stream and waits for them: what W and bias
+ * are made of has to be there by then.
  */
 as_status as_layer_create(as_layer **out, const void *W, int64_t ldw, const void *bias,
                           int32_t n, int32_t k, float scale, as_act act, float act_arg,
@@ -537,10 +538,14 @@ as_status as_layer_destroy(as_layer *layer);
  *   out        DEVICE [rows, n], out_dtype, rows ldo >= n apart; must not overlap x
  *   out_dtype  AS_F32, or AS_BF16 from a bf16 layer
  * Rows may start anywhere; columns n.. of out are not written.  rows may be 0 and
- * at most the context's max_rows.  bf16 rows of x that do not start on 16 bytes,
- * or a k that is no multiple of 64, take room for a copy of x in the context,
- * (re)allocated when a call needs more than any earlier one did, and narrow
- * products 32 MiB once: such a first call must not be made under stream capture.
+ * at most the context's max_rows.  A bf16 x whose rows do not all start on 16
+ * bytes, or a bf16 layer whose k is no multiple of 64, takes room for a copy of x
+ * in the context (rows * k, brought to a multiple of 64, * 2 bytes), which is
+ * (re)allocated when a call needs more than any earlier one did: that call
+ * synchronises the stream, frees what graphs captured earlier work on, and must
+ * not be made under capture.  All other calls allocate nothing.
+ * A call of the same rows, on the same addresses' alignment, gives the same bits
+ * each time; rows do not affect each other (NaN in one leaves the others alone).
  */
 as_status as_linear(as_ctx *ctx, const as_layer *layer, const void *x, int64_t rows,
                     int64_t ldx, const void *residual, int64_t ldr,

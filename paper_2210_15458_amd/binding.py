@@ -335,14 +335,15 @@ def _rows(t, dtype, name, rows, cols):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
-    (r, c), (ld, one) = t.shape, t.stride()
+    r, c = t.size(0), t.size(1)
     if r < rows or c < cols:
         raise ValueError(f"{name} is {r} x {c}, needs {rows} x {cols}")
-    if one != 1 and c > 1:
+    if c > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
     if r < 2:
-        ld = c                            # (one row: its stride says nothing)
-    elif ld < c:
+        return t.data_ptr(), c            # (one row: its stride says nothing)
+    ld = t.stride(0)
+    if ld < c:
         raise ValueError(f"{name} has rows that overlap")
     return t.data_ptr(), ld
 
@@ -413,19 +414,24 @@ def _shaping_ref(shaping, rows, V):
 
 def as_shape_logits(ctx, logits, shaping, logits_out):
     """The first V columns of logits [rows, >= V], shaped, to logits_out (which may be logits)."""
-    rows = logits.shape[0]
-    ptr, ld = _rows(logits, ctx.torch_dtype, "logits", rows, ctx.V)
-    out, ldo = _rows(logits_out, ctx.torch_dtype, "logits_out", rows, ctx.V)
-    ctx._check(lib().as_shape_logits(ctx._h, ptr, rows, ld, _shaping_ref(shaping, rows, ctx.V), out, ldo))
+    rows, V = logits.size(0), ctx.V
+    ptr, ld = _rows(logits, ctx.torch_dtype, "logits", rows, V)
+    out, ldo = _rows(logits_out, ctx.torch_dtype, "logits_out", rows, V)
+    rc = (_lib or lib()).as_shape_logits(ctx._h, ptr, rows, ld, _shaping_ref(shaping, rows, V), out, ldo)
+    if rc:
+        ctx._check(rc)
 
 
 def as_linear(ctx, layer, x, out, residual=None, shaping=None):
-    rows = x.shape[0]
+    """out = act(scale * x W^T + bias) + residual, shaped: the layer's product with all that follows it in one pass."""
+    rows, n, dtype = x.size(0), layer.n, out.dtype
     xp, ldx = _rows(x, layer.torch_dtype, "x", rows, layer.k)
-    op, ldo = _rows(out, out.dtype, "out", rows, layer.n)
-    rp, ldr = (None, 0) if residual is None else _rows(residual, out.dtype, "residual", rows, layer.n)
-    ctx._check(lib().as_linear(ctx._h, layer._h, xp, rows, ldx, rp, ldr,
-                               None if shaping is None else _shaping_ref(shaping, rows, layer.n), op, ldo, _dtype_code(out)))
+    op, ldo = _rows(out, dtype, "out", rows, n)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, dtype, "residual", rows, n)
+    rc = (_lib or lib()).as_linear(ctx._h, layer._h, xp, rows, ldx, rp, ldr, None if shaping is None else _shaping_ref(shaping, rows, n),
+                                   op, ldo, _dtype_code(out))
+    if rc:
+        ctx._check(rc)
 
 
 def as_history_set(ctx, seen, counts, prompts=None, prompt_offsets=None, rows_per_prompt=1, tokens=None, lens=None, which=None):
@@ -446,7 +452,8 @@ def as_history_set(ctx, seen, counts, prompts=None, prompt_offsets=None, rows_pe
 
 
 def as_history_add(ctx, seen, counts, tokens, finished=None):
-    rows = seen.shape[0]
+    """One token more for each row of the record, but for finished rows."""
+    rows = seen.size(0)
     sp, sld = _rows(seen, torch.int32, "seen", rows, (ctx.V + 31) // 32)
     cp, cld = (None, 0) if counts is None else _rows(counts, torch.int32, "counts", rows, ctx.V)
     ctx._check(lib().as_history_add(ctx._h, sp, sld, cp, cld, rows, _dev(tokens, torch.int32, "tokens", rows),

@@ -240,6 +240,9 @@ template <class OutT, int TM, int TN, int KG> struct TileEnd {
 // reads nor the loads meet a bank twice.  Rows past either end repeat the last one and are not stored.
 // v_mfma_f32_32x32x16_bf16 with W as its first operand: register v of lane l is column 8 (v / 4) + 4 (l / 32) + v % 4 and
 // row l % 32 of the 32 x 32, so that a lane holds runs of four consecutive outputs.
+// Bound by the round trips of a step (requests, barrier, fragments, products: some 500 cycles of 64 x 64 against 128 of products), which
+// is why two to five blocks stand on a compute unit where there are tiles for them, and by the launch: 1024 x 512 x 2048 7.6 us (0.28
+// PFLOP/s), 1024 x 2048 x 512 9.7, an empty sum of the size 2.7.  More stages ahead changed nothing (a ring of 6 for 4: 10.6 for 10.1).
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
@@ -397,7 +400,8 @@ __global__ __launch_bounds__(256) void linear_tile(LinearArgs a, uint32_t mtiles
 // Up to 16 rows: a pass over W, each of whose elements one wave needs once, so that LDS would be a detour.  A wave takes 16 columns
 // (v_mfma_f32_16x16x32_bf16, W first: lane l has 8 k from 8 (l / 16) on of row l % 16, and of the result row l % 16, columns
 // 4 (l / 16) .. + 3) and one of KW shares of the sum, with U stages of 64 k, whole lines, on their way at once; the shares meet in
-// LDS, in order.  WAVES / KW column groups a block.
+// LDS, in order.  WAVES / KW column groups a block.  Bound by one round trip to memory beside the launch where W is small (1 x 512 x
+// 2048 3.0 us, an empty launch 2.2), by the memory where it is large (1 x 4096 x 4096 8.1 us, 4.1 TB/s; 1 x 1024 x 256000 79, 6.7).
 template <class OutT, int WAVES, int KW, int U>
 __global__ __launch_bounds__(WAVES * kWave) void linear_few(LinearArgs a)
 {
@@ -470,6 +474,10 @@ __global__ __launch_bounds__(WAVES * kWave) void linear_few(LinearArgs a)
 // tiles.  A stage of 64 KB is requested whole, a request or two between two matrix instructions, into the slot of the ring
 // that the stage before last has just left.  Fragments are read by hand, one between every two matrix instructions, a slice
 // of 16 k ahead; the schedule is pinned.
+//
+// Bound by the matrix instructions under the power limit: 8192 x 4096 x 4096 240 us, 1.15 PFLOP/s (a library product of 8192 cubed on
+// this card 1.25), 16384 x 1024 x 4096 131 us, 1.05; and by what nothing overlaps, a tile's epilogue: with gelu 165, with 66 MB of
+// output for 33 GFLOP 1024 x 512 x 32128 43 (0.79), shaped 80.
 //
 // Tiles stand in bands of eight rows of tiles, and the columns of a band go to the 8 XCDs in turn, as the blocks do: what the 32
 // workers of an XCD have open at a time, 8 row and 4 column tiles, comes into its L2 once, and the XCDs write side by side.
@@ -1135,6 +1143,8 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
 // 4 (l / 16) .. + 3).  Which k are a lane's first to fourth of sixteen does not matter as long as both operands agree, so a
 // lane takes four in a row with one read, of LDS rows 16 bytes longer than they need be (no two lanes of 16 on one bank).
 // Rows of x and W may start anywhere: 16 bytes at a time through registers, the next step's while this one is worked on.
+// Large products run at 70 % of the fp32 matrix rate (2048 x 1024 x 2048 80 us, 107 TFLOP/s), small ones wait for their loads
+// (333 x 515 x 1031 10 us, 16 x 512 x 2048 3.9).
 template <int WM, int WN, int KG, int FM, int FN, int KS>
 __global__ __launch_bounds__(256) void linear_f32(LinearArgs a, uint32_t mtiles, uint32_t ntiles)
 {
@@ -1349,8 +1359,8 @@ static bool big_applies(const as_ctx *ctx, const LinearArgs &a)
 //     128  512  32128    44.7   25.8   13.8   12.6   13.9   22.2
 //    1024  512  32128     390    235   94.4   83.2   93.5   50
 //    4096 1024   4096     249    168   84.0   68.6   73.4   41.0
-// A shaping adds to what a block does behind its sums: 256 x 512 x 32128 39.1 / 29.4 / 53.2 / 45.4 (64, 64 Many, 128, large), 1024 x
-// 512 x 32128 153 / 117 / 211 / 92.
+// A shaping adds to what a block does behind its sums: 64 x 512 x 32128 21.8 / 13.5 / 13.4 / 19.6 / 42.8 (32 Many, 64, 64 Many, 128,
+// large), 256 x 512 x 32128 - / 39.1 / 29.4 / 53.2 / 45.4, 1024 x 512 x 32128 - / 153 / 117 / 211 / 80.
 // Up to 16 rows (us, by 2, 4 and 8 shares of the sum, then 32 Many and 64 Many): 1 x 512 x 2048 3.1 / 3.1 / 4.5 / 3.6 / 4.5, 1 x
 // 512 x 8192 3.8 / 4.7 / 7.3 / 4.6 / 6.3, 1 x 4096 x 4096 16.2 / 9.5 / 8.1 / 13.8 / 29.9, 16 x 2048 x 512 9.0 / 5.8 / 5.9 / 6.3 / 9.9, 1 x
 // 1024 x 256000 85.2 / 78.8 / 152 / 97.3 / 88.9, 16 x 512 x 32128 9.6 / 16.7 / 31.5 / 9.3 / 7.6, 16 x 1024 x 256000 127 / 126 / 230 / 111 / 95.4:
@@ -1370,12 +1380,12 @@ static Form form_of(const as_ctx *ctx, const LinearArgs &a)
     const double u32 = units(32), u64 = units(64), u128 = units(128), u256 = units(256), more = a.shaped ? 1.0 : 0.0;
     const double few = u64 < 5 ? u64 : 5, full = (double)((a.rows + 255) / 256) * (double)((a.n + 255) / 256) / cus;
     const double t[] = {
-        1.2 + u32 * (1.2 + 0.16 * S),
-        1.2 + (u32 <= 1 ? 0.7 : ceil(u32 / 2)) * (0.9 + 0.26 * S),
+        1.2 + u32 * (1.2 + 0.16 * S) + more * (4.0 + 0.6 * u32),
+        1.2 + (u32 <= 1 ? 0.7 : ceil(u32 / 2)) * (0.9 + 0.26 * S) + more * (4.0 + 0.6 * u32),
         2.6 + 0.26 * S + (u64 - 1) * (0.9 + 0.235 * S) + more * (4.5 + 1.85 * u64),
         2.2 + 0.46 * S + (few - 1) * (0.6 + 0.14 * S) + (u64 - few) * (0.75 + 0.225 * S) + more * (4.0 + u64),
         1.0 + u128 * (7.2 + 0.6 * S + 15.0 * more),
-        5.0 + u256 * (4.0 + 1.1 * S + 0.7 * S * (full < 1 ? full : 1) + 20.0 * more),
+        5.0 + u256 * (4.0 + 1.1 * S + 0.7 * S * (full < 1 ? full : 1) + 17.0 * more),
     };
     int best = 0;
     for (int f = 1; f < 6; ++f)

@@ -15,6 +15,9 @@ namespace as {
 // of one or two lanes of its wave.  So the seen columns are listed in LDS first, their counts fetched by the list, all at
 // once, and what each is to lose (frequency * count, and presence) left in its place, where the column's lane finds it
 // by the number of seen columns before it.  Where more are seen than the list holds, the lanes read all their counts.
+// Bound by the memory: 1024 x 32128 bf16 in and out 28 us without penalties (4.7 TB/s), 1024 x 256000 170 (6.2); the counts add a line of
+// 128 bytes for each seen token that no other shares one with: with 16, 64, 256, 2000 tokens counted and as many of a prompt 32,
+// 34, 44, 51 us, and with all modifiers 48 (256 of either) and 263 (512).
 constexpr int kListed = 256;
 template <class T, int P, bool NT>
 __global__ __launch_bounds__(256) void shape_kernel(as_shaping s, const T *in, int64_t rows, int64_t ld, T *out, int64_t ldo,
@@ -152,7 +155,9 @@ as_status launch_shape(as_ctx *ctx, const as_shaping &s, const void *logits, int
 // (whole numbers: the order of the additions does not matter), then writes the slice's words of bits, a lane each, and the
 // counts of those tokens that are or were seen; all others are zero and stay so.  So the counts, 4 bytes a token of the
 // vocabulary, are touched only where something is, and a launch needs nothing cleared before it.  Every block
-// reads its rows' whole lists: they are short beside the record, and come from the caches.
+// reads its rows' whole lists: they are short beside the record, and come from the caches.  16 prompts of up to 512 tokens, 64 rows
+// each with up to 64 of its own, V = 32128: 18 us, a chain of a few round trips a row, four rows a block; 16 rows of a prompt of up
+// to 32768 with up to 4096 of their own, V = 256000: 12 us, which every block reads.
 constexpr int kSlice = 8192;
 
 // A token's count in LDS: the 32 of a word turned by the word's number, so that lanes at one bit of their words meet no bank twice
