@@ -156,8 +156,9 @@ as_status launch_shape(as_ctx *ctx, const as_shaping &s, const void *logits, int
 // counts of those tokens that are or were seen; all others are zero and stay so.  So the counts, 4 bytes a token of the
 // vocabulary, are touched only where something is, and a launch needs nothing cleared before it.  Every block
 // reads its rows' whole lists: they are short beside the record, and come from the caches.  16 prompts of up to 512 tokens, 64 rows
-// each with up to 64 of its own, V = 32128: 18 us, a chain of a few round trips a row, four rows a block; 16 rows of a prompt of up
-// to 32768 with up to 4096 of their own, V = 256000: 12 us, which every block reads.
+// each with up to 64 of its own, V = 32128: 18 us, four rows a block; 16 rows of a prompt of up
+// to 32768 with up to 4096 of their own, V = 256000: 12 us, which every block reads.  Slices of 4096: 24 and 18 us, of 16384 the
+// same as these; a row's old words and tokens asked for a row ahead: the same.
 constexpr int kSlice = 8192;
 
 // A token's count in LDS: the 32 of a word turned by the word's number, so that lanes at one bit of their words meet no bank twice
