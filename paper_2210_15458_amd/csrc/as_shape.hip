@@ -223,14 +223,16 @@ __global__ __launch_bounds__(WAVES * kWave) void history_set_kernel(HistoryArgs 
         if (tid < kWords) bits[tid] = 0;
         for (int v = tid * 4; v < kSlice; v += WAVES * kWave * 4) *reinterpret_cast<uint4 *>(count + v) = uint4{0, 0, 0, 0};
         __syncthreads();
+        uint32_t of_prompt = 0;
         if (a.prompts) {
             int64_t from = scalar_load(a.offsets + p), to = scalar_load(a.offsets + p + 1);
             from = from > 0 ? from : 0;
             to = to < a.prompts_len ? to : a.prompts_len;
             if (from < to) tally<false>(a.prompts + from, to - from, first, width, bits, count);
             __syncthreads();
+            if (tid < kWords) of_prompt = bits[tid];
+            __syncthreads();                                          // (before the first row's own tokens are marked in the same words)
         }
-        const uint32_t of_prompt = tid < kWords ? bits[tid] : 0u;
         for (int64_t row = row0; row < row1; ++row) {
             if (a.which && !a.which[row]) continue;                   // (the same for the whole block)
             uint32_t *const words = a.seen + row * a.seen_ld + first / 32;
