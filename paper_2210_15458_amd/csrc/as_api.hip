@@ -1200,7 +1200,9 @@ as_status as_history_set(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
     if (tokens && (T < 0 || tokens_ld < T)) return fail(ctx, AS_ERR_INVALID_ARG, "tokens need T >= 0 and tokens_ld >= T");
     HistoryArgs a{};
     a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V; a.which = which;
-    a.prompts = prompts; a.offsets = prompt_offsets; a.prompts_len = prompts_len; a.per = prompts ? rows_per_prompt : 1;
+    a.prompts = prompts; a.offsets = prompt_offsets; a.prompts_len = prompts_len;
+    // (a prompt's rows past the last one would be launched for nothing: 2^31 of them, if it says so)
+    a.per = !prompts ? 1 : rows_per_prompt < rows ? rows_per_prompt : (int32_t)rows;
     a.tokens = tokens; a.tokens_ld = tokens_ld; a.T = T; a.lens = lens;
     return launch_history_set(ctx, a);
 }

@@ -220,6 +220,7 @@ __global__ __launch_bounds__(WAVES * kWave) void history_set_kernel(HistoryArgs 
         const int64_t p = item / groups, row0 = p * a.per + (item - p * groups) * group;
         int64_t row1 = row0 + group < (p + 1) * a.per ? row0 + group : (p + 1) * a.per;
         row1 = row1 < a.rows ? row1 : a.rows;
+        if (row0 >= row1) continue;                                   // (the last prompt may have fewer rows)
         if (tid < kWords) bits[tid] = 0;
         for (int v = tid * 4; v < kSlice; v += WAVES * kWave * 4) *reinterpret_cast<uint4 *>(count + v) = uint4{0, 0, 0, 0};
         __syncthreads();

@@ -56,3 +56,18 @@ def test_rows_that_share_a_block(rows, per, V, P, T):
         want_counts = c if want_counts is None else np.where(live, c, want_counts)
         assert torch.equal(seen, pack(want_seen)), turn
         assert torch.equal(counts, dev(want_counts)), turn
+
+
+@pytest.mark.parametrize("rows,V", [(16, 32128), (600, 70001)])
+@pytest.mark.parametrize("past", [1, 1000, 2 ** 31 - 1])
+def test_rows_per_prompt_beyond_the_rows(rows, V, past):
+    """One prompt for all, said as a number of rows that there are not: the rows that are there are all that is worked on."""
+    per = past if past > rows else rows + past
+    rng = np.random.default_rng(rows)
+    seen, counts = record(rows, V)
+    pt, offsets = ragged(rng, 1, 4000, V)
+    tt = own_tokens(rng, rows, V, 25)
+    print(f"rows {rows} of {per}, V {V}", flush=True)
+    B.as_history_set(B.Ctx(rows, V, torch.float32), seen, counts, dev(pt), dev(offsets), per, dev(tt))
+    want_seen, want_counts = history64(rows, V, pt, offsets, per, tt, np.full(rows, 25))
+    assert torch.equal(seen, pack(want_seen)) and torch.equal(counts, dev(want_counts))
