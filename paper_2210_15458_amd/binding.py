@@ -349,7 +349,11 @@ def _rows(t, dtype, name, rows, cols):
 
 
 class Layer:
-    """as_layer: act(scale * x W^T + bias) for W [n, k] (borrows W where the library does not lay it out anew)."""
+    """as_layer: act(scale * x W^T + bias) for W [n, k].
+
+    Made of W and bias as the current stream leaves them, which is waited for (the library reads them on another).  The bias is
+    copied, and W if it is bf16 and k no multiple of 64 or its rows do not start on 16 bytes: later changes do not show.  Any
+    other W is borrowed: it is kept alive, and what is written to it later shows in the calls behind that."""
 
     def __init__(self, W, bias=None, act="none", act_arg=0.0, scale=1.0):
         if not isinstance(W, torch.Tensor) or W.dim() != 2:
@@ -361,8 +365,9 @@ class Layer:
         self._W = W                       # keep the borrowed tensor alive
         self._h = C.c_void_p()
         ptr, ld = _rows(W, W.dtype, "W", self.n, self.k)
-        rc = lib().as_layer_create(C.byref(self._h), ptr, ld, _dev(bias, W.dtype, "bias", self.n), self.n, self.k, float(scale),
-                                   ACTS[act], float(act_arg), _dtype_code(W))
+        bias, dtype = _dev(bias, W.dtype, "bias", self.n), _dtype_code(W)
+        torch.cuda.current_stream(W.device).synchronize()
+        rc = lib().as_layer_create(C.byref(self._h), ptr, ld, bias, self.n, self.k, float(scale), ACTS[act], float(act_arg), dtype)
         if rc != 0:
             raise ArithSamplingError(rc, (lib().as_last_error(None) or b"").decode())
 
