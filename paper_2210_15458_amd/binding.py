@@ -171,7 +171,7 @@ class Ctx:
 
 
 class Model:
-    """as_model: the synthetic low-rank bigram model (borrows E, re-lays U out)."""
+    """as_model: the synthetic low-rank bigram model (borrows E, re-lays U out as the current stream leaves it, which is waited for)."""
 
     def __init__(self, E, U, scale=3.0):
         V, d = E.shape
@@ -182,8 +182,9 @@ class Model:
         self.V, self.d = int(V), int(d)
         self._E = E                       # keep the borrowed tensor alive
         self._h = C.c_void_p()
-        rc = lib().as_model_create_bigram(C.byref(self._h), _dev(E, E.dtype, "E"), _dev(U, U.dtype, "U"),
-                                          self.V, self.d, float(scale), _dtype_code(E))
+        e, u, dtype = _dev(E, E.dtype, "E"), _dev(U, U.dtype, "U"), _dtype_code(E)
+        torch.cuda.current_stream(E.device).synchronize()
+        rc = lib().as_model_create_bigram(C.byref(self._h), e, u, self.V, self.d, float(scale), dtype)
         if rc != 0:
             raise ArithSamplingError(rc, (lib().as_last_error(None) or b"").decode())
 

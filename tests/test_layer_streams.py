@@ -1,4 +1,4 @@
-"""A Layer is made of tensors that the current stream may still be filling: the binding waits for that stream before the library,
+"""A Layer, as a Model, is made of tensors that the current stream may still be filling: the binding waits for that stream before the library,
 which reads them on another, is called (seen here without a GPU, by the order of the calls)."""
 import pytest
 import torch
@@ -25,6 +25,8 @@ class Library:
 
     def as_layer_destroy(self, h):
         return 0
+
+    as_model_create_bigram, as_model_destroy = as_layer_create, as_layer_destroy
 
 
 class Stream:
@@ -53,3 +55,8 @@ def test_nothing_is_waited_for_in_vain(calls):
     with pytest.raises(ValueError):
         B.Layer(on_gpu(4, 64), bias=on_gpu(3))
     assert calls == []
+
+
+def test_a_model_s_too(calls):
+    B.Model(on_gpu(8, 64), on_gpu(64, 8))
+    assert calls == ["wait", "create"]
