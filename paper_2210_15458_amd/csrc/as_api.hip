@@ -195,6 +195,8 @@ static as_status check_shaping(as_ctx *ctx, const as_shaping *given, int64_t row
     else if (!s->seen) return fail(ctx, AS_ERR_INVALID_ARG, "repetition, presence and frequency need seen");
     if (!s->presence && !s->frequency) s->counts = nullptr;
     else if (!s->counts) return fail(ctx, AS_ERR_INVALID_ARG, "presence and frequency need counts");
+    if (!s->bias) s->bias_ids = nullptr;
+    if (!s->mask) s->mask_ids = nullptr;
     if (s->seen) {
         const as_status st = check_record(ctx, s->seen, s->seen_ld, s->counts, s->counts_ld, V);
         if (st != AS_OK) return st;
