@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdlib.h>
 
+#include <initializer_list>
+
 #include <mutex>
 #include <new>
 
@@ -187,6 +189,15 @@ static as_status check_record(as_ctx *ctx, const void *seen, int64_t seen_ld, co
     return AS_OK;
 }
 
+// Whether all of them (NULL among them) lie on whole elements of `size` bytes: the kernels read many by scalar loads, which
+// ignore an address's last bits.
+static bool all_aligned(size_t size, std::initializer_list<const void *> pointers)
+{
+    for (const void *p : pointers)
+        if (reinterpret_cast<uintptr_t>(p) % size != 0) return false;
+    return true;
+}
+
 // A shaping of `rows` rows of V logits: checked, and `s` without the members that nothing in it uses.
 static as_status check_shaping(as_ctx *ctx, const as_shaping *given, int64_t rows, int32_t V, as_shaping *s)
 {
@@ -213,6 +224,8 @@ static as_status check_shaping(as_ctx *ctx, const as_shaping *given, int64_t row
             return fail(ctx, AS_ERR_INVALID_ARG, "mask_rows must be 1, or a row for each where mask_ids is NULL");
         if (reinterpret_cast<uintptr_t>(s->mask) % 4 != 0) return fail(ctx, AS_ERR_INVALID_ARG, "mask is not aligned to its element type");
     }
+    if (!all_aligned(4, {s->repetition, s->presence, s->frequency, s->bias_ids, s->mask_ids}))
+        return fail(ctx, AS_ERR_INVALID_ARG, "repetition, presence, frequency, bias_ids or mask_ids is not aligned to its element type");
     return AS_OK;
 }
 
@@ -1200,6 +1213,8 @@ as_status as_history_set(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
     if (prompts && (!prompt_offsets || prompts_len < 0 || rows_per_prompt < 1))
         return fail(ctx, AS_ERR_INVALID_ARG, "prompts need prompt_offsets, prompts_len >= 0 and rows_per_prompt >= 1");
     if (tokens && (T < 0 || tokens_ld < T)) return fail(ctx, AS_ERR_INVALID_ARG, "tokens need T >= 0 and tokens_ld >= T");
+    if (!all_aligned(4, {prompts, tokens, tokens ? lens : nullptr}) || !all_aligned(8, {prompts ? prompt_offsets : nullptr}))
+        return fail(ctx, AS_ERR_INVALID_ARG, "prompts, prompt_offsets, tokens or lens is not aligned to its element type");
     HistoryArgs a{};
     a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V; a.which = which;
     a.prompts = prompts; a.offsets = prompt_offsets; a.prompts_len = prompts_len;
@@ -1215,6 +1230,7 @@ as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
     const as_status st = check_history(ctx, seen, seen_ld, counts, counts_ld, rows);
     if (st != AS_OK || rows == 0) return st;
     if (!tokens) return fail(ctx, AS_ERR_INVALID_ARG, "tokens must not be NULL");
+    if (!all_aligned(4, {tokens})) return fail(ctx, AS_ERR_INVALID_ARG, "tokens is not aligned to its element type");
     HistoryArgs a{};
     a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V;
     return launch_history_add(ctx, a, tokens, finished);
