@@ -447,8 +447,8 @@ def as_history_set(ctx, seen, counts, prompts=None, prompt_offsets=None, rows_pe
     cp, cld = (None, 0) if counts is None else _rows(counts, torch.int32, "counts", rows, ctx.V)
     pp, po, plen = None, None, 0
     if prompts is not None:
-        plen, pp = prompts.numel(), _dev(prompts, torch.int32, "prompts")
-        po = _dev(prompt_offsets, torch.int64, "prompt_offsets", (rows - 1) // int(rows_per_prompt) + 2)
+        plen, pp, per = prompts.numel(), _dev(prompts, torch.int32, "prompts"), int(rows_per_prompt)
+        po = _dev(prompt_offsets, torch.int64, "prompt_offsets", (rows - 1) // per + 2 if per > 0 else None)
     tp, tld, T = None, 0, 0
     if tokens is not None:
         tp, tld = _rows(tokens, torch.int32, "tokens", rows, 0)

@@ -50,3 +50,12 @@ def test_a_history_s_lists(name, shift):
         refused(ctx, B.lib().as_history_add(ctx._h, seen.data_ptr(), 4, counts.data_ptr(), V, ROWS, at["tokens"], None), "aligned")
     torch.cuda.synchronize()
     assert not bool(seen.any()) and not bool(counts.any())
+
+
+@pytest.mark.parametrize("per", [0, -1, -7])
+def test_rows_per_prompt(per):
+    ctx = B.Ctx(ROWS, V, torch.float32)
+    seen = ints(ROWS, 4)
+    with pytest.raises(B.ArithSamplingError, match="rows_per_prompt"):
+        B.as_history_set(ctx, seen, None, ints(5), torch.zeros(9, dtype=torch.int64, device="cuda"), per)
+    assert not bool(seen.any())
