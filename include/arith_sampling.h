@@ -445,8 +445,11 @@ as_status as_encode(as_ctx *ctx, const as_model *model, const int32_t *prompts,
  * on the logits before they are sampled from (as_shape_logits, or the last
  * layer's as_linear with a shaping), and the record of each sequence's tokens
  * that the penalties among them go by (as_history_set, as_history_add).
- * All of them work on the context's stream; none looks at the context's
- * vocabulary but as_shape_logits.
+ * All of them work on the context's stream.  as_linear does not look at the
+ * context's vocabulary (its outputs are the layer's n); as_shape_logits and the
+ * histories work on rows of it, and as_history_set and as_history_add leave out
+ * tokens past it: a context made for layers alone, with some small vocabulary,
+ * is none for them.
  */
 typedef struct as_layer as_layer;
 
@@ -556,7 +559,8 @@ as_status as_linear(as_ctx *ctx, const as_layer *layer, const void *x, int64_t r
  * The record that repetition, frequency and presence go by, of `rows` sequences:
  * which tokens each has seen, and how often it has emitted each, in buffers of
  * the caller's (seen and counts as in as_shaping) that start out as zeros and are
- * then changed by these two calls alone.  V is the context's.
+ * then changed by these two calls alone, with counts in every one of them or
+ * (NULL) in none.  V is the context's.
  *
  * as_history_set: row r's record becomes that of its prompt and its own tokens.
  * Tokens of the prompt are seen, the row's own are seen and counted.

@@ -71,3 +71,19 @@ def test_rows_per_prompt_beyond_the_rows(rows, V, past):
     B.as_history_set(B.Ctx(rows, V, torch.float32), seen, counts, dev(pt), dev(offsets), per, dev(tt))
     want_seen, want_counts = history64(rows, V, pt, offsets, per, tt, np.full(rows, 25))
     assert torch.equal(seen, pack(want_seen)) and torch.equal(counts, dev(want_counts))
+
+
+def test_the_context_s_vocabulary():
+    """Tokens past the context's vocabulary are left out, whatever the buffers have room for; a layer does not look at it."""
+    rows, V, room = 5, 100, 1000
+    seen, counts = record(rows, room)
+    ctx = B.Ctx(rows, V, torch.float32)
+    tt = dev(np.tile(np.array([[3, 99, 100, 999]], dtype=np.int32), (rows, 1)))
+    B.as_history_set(ctx, seen, counts, tokens=tt)
+    B.as_history_add(ctx, seen, counts, torch.full((rows,), 500, dtype=torch.int32, device="cuda"))
+    want = np.zeros((rows, room), dtype=np.int32)
+    want[:, [3, 99]] = 1
+    assert torch.equal(counts, dev(want)) and torch.equal(seen, pack(want > 0))
+    out = torch.empty(rows, room, device="cuda")
+    B.as_linear(ctx, B.Layer(torch.ones(room, 8, device="cuda")), torch.ones(rows, 8, device="cuda"), out)
+    assert bool((out == 8.0).all())
