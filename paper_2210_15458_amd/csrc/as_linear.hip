@@ -1063,6 +1063,7 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
     bf16x8 xa[2], wa[4], xb[2], wb[4];
     AS_RX(xa, 0, 0u, 0); AS_RX(xa, 1, 0u, 0);
     AS_RW(wa, 0, 0u, 0); AS_RW(wa, 1, 0u, 0); AS_RW(wa, 2, 0u, 0); AS_RW(wa, 3, 0u, 0);
+    AS_WAIT(xa, wa);
     int gs = 0;                                                       // stages worked on: stage gs lies in slot gs & 1
     int stores = 0;                                                   // of the tile before, behind the requests for this one
     for (uint32_t j = 0; j < tiles; ++j) {
@@ -1122,10 +1123,12 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
         const uint32_t stage = lds0 + 2 * kBigRing + (uint32_t)wave * kBigStage;
         if constexpr (FORM == 2) stores = shaped_epilogue<OutT>(a, acc, stage, m0 + wm * 64, n0 + wn * 128, lane);
         else stores = big_epilogue<OutT, FORM>(a, acc, stage, m0 + wm * 64, n0 + wn * 128, lane);
-        // the first fragments of the next tile, again: they do not take the epilogue's registers
+        // the first fragments of the next tile, again (behind the last tile for nothing): they do not take the epilogue's registers.
+        // Waited for here: no read is in flight across the loop's end, where the compiler may move registers, or when the wave ends.
         const uint32_t so = (uint32_t)(gs & 1) * kBigRing;
         AS_RX(xa, 0, so, 0); AS_RX(xa, 1, so, 0);
         AS_RW(wa, 0, so, 0); AS_RW(wa, 1, so, 0); AS_RW(wa, 2, so, 0); AS_RW(wa, 3, so, 0);
+        AS_WAIT(xa, wa);
     }
 #undef AS_SB
 #undef AS_RQ
