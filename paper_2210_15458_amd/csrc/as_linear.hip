@@ -28,14 +28,27 @@ __device__ __forceinline__ float tanh_for_bf16(float x)
     return fabsf(x) < 0.03125f ? fmaf(x * (-1.f / 3.f), x * x, x) : y;
 }
 
-// erf by Abramowitz and Stegun 7.1.26 (1.5e-7 off at most): erfc x = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x >= 0.
-// z/2 (1 + erf(z / sqrt 2)) = z h or z (1 - h) with h = erfc(|z| / sqrt 2) / 2: no cancellation in the lower tail.
-__device__ __forceinline__ float gelu_of(float z)
+// z/2 (1 + erf(z / sqrt 2)) = z h or z (1 - h) with h = erfc(|z| / sqrt 2) / 2 = t P(t) e^(-z^2 / 2), t = 1 / (1 + p |z| / sqrt 2): no
+// cancellation in the lower tail.  For outputs rounded to bf16 P is Abramowitz and Stegun 7.1.26, five terms, 7.5e-8 off at most (of
+// h itself: 5e-4 at z = -4).  For fp32 outputs nine terms with p = 0.37, fitted by reweighted least squares to the smallest relative error
+// over |z| < 13, 1.7e-8: what remains is the roundings', 4e-7 of the result at -1, 1.4e-6 at -5, where the argument of e is rounded.
+template <class OutT> __device__ __forceinline__ float gelu_of(float z)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, fabsf(z), 1.f));
+    constexpr bool SHORT = sizeof(OutT) == 2;
+    const float t = __builtin_amdgcn_rcpf(fmaf((SHORT ? 0.3275911f : 0.37f) * 0.70710678118654752440f, fabsf(z), 1.f));
     const float e = __builtin_amdgcn_exp2f(-0.72134752044448170368f * (z * z));
-    const float c = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f), 0.5f * 1.421413741f),
-                                     -0.5f * 0.284496736f), 0.5f * 0.254829592f);
+    float c;
+    if constexpr (SHORT) {
+        c = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f), 0.5f * 1.421413741f),
+                             -0.5f * 0.284496736f), 0.5f * 0.254829592f);
+    } else {
+        constexpr float P[9] = {0.10440687f, 0.10371493f, 0.10312697f, 0.053260326f, 0.15540063f,
+                                -0.14265543f, 0.2434205f, -0.15163632f, 0.030961514f};
+        c = P[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i) c = fmaf(t, c, P[i]);
+        c *= t;
+    }
     const float h = c * e;
     return z * (z > 0.f ? 1.f - h : h);
 }
@@ -50,7 +63,7 @@ template <class OutT, int N, class V> __device__ __forceinline__ void activate(V
         break;
     case AS_ACT_GELU:
 #pragma unroll
-        for (int e = 0; e < N; ++e) z[e] = gelu_of(z[e]);
+        for (int e = 0; e < N; ++e) z[e] = gelu_of<OutT>(z[e]);
         break;
     case AS_ACT_GELU_TANH:                                            // z/2 (1 + tanh u) = z / (1 + e^-2u)
 #pragma unroll
