@@ -506,8 +506,8 @@ typedef struct as_shaping {
 
 /*
  * logits_out[r, :V] = logits[r, :V] shaped, rounded once to the context's
- * logits dtype.  logits_out may be logits (same ld_out); otherwise the two must
- * not overlap.  Rows may start anywhere and be any stride >= V apart; columns
+ * logits dtype.  logits_out may be logits (with its ld, or one row); otherwise
+ * the two must not overlap.  Rows may start anywhere and be any stride >= V apart; columns
  * V.. of a row are neither read nor written.
  */
 as_status as_shape_logits(as_ctx *ctx, const void *logits, int64_t rows, int64_t ld,
@@ -536,7 +536,7 @@ as_status as_layer_destroy(as_layer *layer);
  * matrix instructions, an fp32 layer's on the fp32 ones.
  *   x          DEVICE [rows, k], the layer's wdtype, rows ldx >= k apart
  *   residual   DEVICE [rows, n], out_dtype, rows ldr >= n apart, or NULL; may be
- *              `out` itself (ldr = ldo)
+ *              `out` itself (ldr = ldo, or one row)
  *   shaping    or NULL
  *   out        DEVICE [rows, n], out_dtype, rows ldo >= n apart; must not overlap x
  *   out_dtype  AS_F32, or AS_BF16 from a bf16 layer

@@ -1096,7 +1096,7 @@ as_status as_shape_logits(as_ctx *ctx, const void *logits, int64_t rows, int64_t
     if (rows == 0) return AS_OK;
     if (!logits || !logits_out) return fail(ctx, AS_ERR_INVALID_ARG, "logits and logits_out must not be NULL");
     if (ld < ctx->V || ld_out < ctx->V) return fail(ctx, AS_ERR_INVALID_ARG, "ld is smaller than the vocabulary");
-    if (logits == logits_out && ld != ld_out) return fail(ctx, AS_ERR_INVALID_ARG, "logits shaped in place with another ld_out");
+    if (logits == logits_out && ld != ld_out && rows > 1) return fail(ctx, AS_ERR_INVALID_ARG, "logits shaped in place with another ld_out");
     if (!aligned_to(logits, ctx->dtype) || !aligned_to(logits_out, ctx->dtype))
         return fail(ctx, AS_ERR_INVALID_ARG, "logits pointer is not aligned to its element type");
     as_shaping s;
@@ -1177,7 +1177,7 @@ as_status as_linear(as_ctx *ctx, const as_layer *layer, const void *x, int64_t r
         return fail(ctx, AS_ERR_INVALID_ARG, "ldx, ldr or ldo is smaller than its rows");
     if (!aligned_to(x, layer->wdtype) || !aligned_to(out, out_dtype) || !aligned_to(residual, out_dtype))
         return fail(ctx, AS_ERR_INVALID_ARG, "x, residual or out is not aligned to its element type");
-    if (residual == out && ldr != ldo) return fail(ctx, AS_ERR_INVALID_ARG, "a residual added in place has the stride of out");
+    if (residual == out && ldr != ldo && rows > 1) return fail(ctx, AS_ERR_INVALID_ARG, "a residual added in place has the stride of out");
     LinearArgs a{};
     a.x = x; a.rows = rows; a.ldx = ldx; a.W = layer->W; a.ldw = layer->ldw; a.n = layer->n; a.k = layer->k;
     a.bias = layer->bias; a.scale = layer->scale; a.act = layer->act; a.act_arg = layer->act_arg;
