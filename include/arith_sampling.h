@@ -477,8 +477,9 @@ typedef enum {
  *   seen, seen_ld       uint32[rows, seen_ld]: token v is bit v % 32 of word
  *                       v / 32; seen_ld >= ceil(V / 32); bits past V are ignored.
  *                       Needed with any of the three strengths.
- *   counts, counts_ld   int32[rows, counts_ld], counts_ld >= V; read only where
- *                       the seen bit is set.  Needed with frequency or presence.
+ *   counts, counts_ld   int32[rows, counts_ld], counts_ld >= V; a count says
+ *                       nothing where the seen bit is not set.  Needed with
+ *                       frequency or presence.
  *   repetition          float[rows], each > 0
  *   presence, frequency float[rows]
  *   bias, bias_ld, bias_rows   float[bias_rows, bias_ld], bias_ld >= V
