@@ -155,7 +155,7 @@ as_status as_ctx_set_tuning(as_ctx *ctx, as_tuning knob, int32_t value);
  * as_ctx_profile_read synchronises the stream, returns the summed kernel time
  * and the number of timed launches since the last read for
  *   kernel 0: fused sampling step   1: logits (bigram) and layers   2: threshold   3: interval (encode) step
- * and resets the counters.  (A decode that makes the logits rows of all tokens before its
+ * and resets the counters.  as_shape_logits, the histories and the copy of x that some layers take are not among them.  (A decode that makes the logits rows of all tokens before its
  * first step has that launch under 1, what it makes of the rows under 2, and its steps, which
  * share one launch, under 0; one that makes rows for the tokens that come has these a few times
  * over.  Profiling changes nothing of what a call launches.)  At most 16384 launches per kernel are timed between

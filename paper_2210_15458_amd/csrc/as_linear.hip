@@ -132,8 +132,8 @@ __device__ __forceinline__ void finish8_sums(const LinearArgs &a, int64_t row, i
     finish8<OutT>(a, row, col, z);
 }
 
-// What a thread finishes, eight columns of a row, whose own loads go out in two rounds, beside the products where they can:
-// what the row and the columns say, and what that points to.
+// What a thread finishes, eight columns of a row, whose own loads go out in two rounds: what the row and the columns say, ahead of
+// the products, and what that points to, in the few-rows form between them, in the tiles behind the last.
 template <class OutT> struct Unit {
     int64_t row;
     int32_t col;
@@ -184,7 +184,7 @@ template <class OutT> struct Unit {
 };
 
 // What 256 threads finish of a tile of TM x TN: each always the same eight columns, of rows 256 / kAcross apart; two of them have
-// their loads out beside the products.  The sums lie in LDS, KG shares of TM rows, kStride floats apart, added in order.
+// their first loads out ahead of the products.  The sums lie in LDS, KG shares of TM rows, kStride floats apart, added in order.
 template <class OutT, int TM, int TN, int KG> struct TileEnd {
     static constexpr int kAcross = TN / 8, kUnits = TM * kAcross > 256 ? TM * kAcross / 256 : 1, kAhead = kUnits < 2 ? 1 : 2;
     static constexpr int kStride = TN + 4, kBytes = KG * TM * kStride * 4;
@@ -1099,7 +1099,8 @@ __global__ __launch_bounds__(512, 1) void linear_big(LinearArgs a, uint32_t mtil
             AS_SLICE(xa, wa, xb, wb, so, 3);
             AS_WAIT(xb, wb);
             // every wave has read all of this stage, and the next one has landed; the stores of the tile before, which were
-            // requested after it, may drain on
+            // requested after it, may drain on (not in the shaped form, which keeps four registers in memory over the products:
+            // the compiler waits for them here, and for the stores with them)
             if (s == 0 && stores == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
             else if (s == 0 && stores == 32) asm volatile("s_waitcnt vmcnt(32)" ::: "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
