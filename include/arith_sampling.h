@@ -593,6 +593,115 @@ as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
                          int64_t counts_ld, int64_t rows, const int32_t *tokens,
                          const uint8_t *finished);
 
+/* ------------------------------------------------ a cache and the attention that reads it */
+
+/*
+ * What a decode with a model that attends to its context needs besides layers:
+ * a cache of keys and values in pages (as_cache_add), the attention of one new
+ * token a row (as_attend), and that of whole prompts or the next chunks of them
+ * (as_attend_prompts).  They work on the context's stream and do not look at its
+ * vocabulary and logits dtype.
+ *
+ *   k, v       DEVICE [pages, kv_heads, page_size, head_dim], dtype, a page page_ld
+ *              elements behind the one before; both on 16 bytes, and so each page
+ *   page_size  tokens of a page: a power of two, at most AS_MAX_PAGE.  From 16 on
+ *              the attention runs faster
+ *   head_dim   a multiple of 8, at most AS_MAX_HEAD_DIM.  64, 128 and 256 run a
+ *              little faster than others
+ */
+#define AS_MAX_PAGE (1 << 20)
+#define AS_MAX_HEADS 1024
+#define AS_MAX_HEAD_DIM 256
+typedef struct as_cache {
+    void *k, *v;
+    int64_t pages, page_ld;
+    int32_t page_size, kv_heads, head_dim;
+    as_dtype dtype;
+} as_cache;
+
+/*
+ * The sequences of a batch: row r's tokens are those of its prompt, which it
+ * shares with the other rows of that prompt, and behind them its own.  Both are
+ * named by tables of pages: token t of a table's row lies in slot t % page_size of
+ * page table[t / page_size].
+ *   table, table_ld   DEVICE int32[rows, table_ld], or NULL: no row has tokens of its own
+ *   lens              DEVICE int32[rows]: how many it has, what a call adds or asks
+ *                     for among them (below 0: 0; above table_ld * page_size: that many)
+ *   prompt_table, prompt_table_ld, prompt_lens, rows_per_prompt
+ *                     the same of prompts: row r has that of r / rows_per_prompt;
+ *                     prompt_table may be NULL: none
+ *   finished          DEVICE uint8[rows] or NULL: rows with a non-zero flag are left
+ *                     out: nothing of theirs is written
+ * Table entries past a length are not looked at.  An entry outside [0, pages) is not
+ * detected: as_cache_add leaves its tokens out, the others read some page.
+ */
+typedef struct as_sequences {
+    const int32_t *table;
+    int64_t table_ld;
+    const int32_t *lens;
+    const int32_t *prompt_table;
+    int64_t prompt_table_ld;
+    const int32_t *prompt_lens;
+    int32_t rows_per_prompt;
+    const uint8_t *finished;
+} as_sequences;
+
+/*
+ * Keys and values of new tokens, the last of their rows' own: `lens` counts them
+ * already.  (It is the caller's to count up, once a step, not once a layer.)  Row r
+ * has the tokens offsets[r] .. offsets[r+1]; without offsets there is one a row.
+ * Prompts are added by sequences of their own, whose table is the prompts'.
+ *   k, v       DEVICE [tokens, kv_heads, head_dim], the cache's dtype, rows ldk and
+ *              ldv >= kv_heads * head_dim apart; may start anywhere
+ *   tokens     at most the context's max_rows (as rows)
+ *   offsets    DEVICE int64[rows + 1], not falling, or NULL (then tokens = rows)
+ * Tokens that the table has no room for, and those before offsets[0] or from
+ * offsets[rows] on, are left out.  No two rows may have a page in common that both
+ * write to.  Allocates nothing.
+ */
+as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
+                       int64_t rows, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                       int64_t tokens, const int64_t *offsets);
+
+/*
+ * One query a row, of the row's last token:
+ *     out[r, h] = sum_j p_j v_j,   p = softmax_j(scale * q[r, h] . k_j)
+ * over the row's tokens j, its prompt's and its own, keys and values of head
+ * h / (heads / kv_heads).  With window > 0 those of the last `window` tokens (itself
+ * among them) and of the sequence's first `sinks` (>= 0); window <= 0: all.  Zeros
+ * where a row has no tokens.  What is not seen does not count, NaN and infinities
+ * among it.  Scores, weights and sums in fp32; products of a bf16 cache by the bf16
+ * matrix instructions, for which the weights are rounded to bf16; rounded once to
+ * the cache's dtype.
+ *   q, out     DEVICE [rows, heads, head_dim], the cache's dtype, rows ldq and ldo >=
+ *              heads * head_dim apart; may start anywhere
+ *   heads      a multiple of kv_heads, at most AS_MAX_HEADS
+ * The keys are split over the GPU where there are few rows, and those of prompts
+ * taken for all their rows together: what the parts come to lies in a workspace of
+ * the context, which is (re)allocated when a call needs more than any earlier one
+ * did; that call synchronises the stream, frees what graphs captured earlier work
+ * on, and must not be made under capture.  What a call needs goes by its sizes
+ * alone (rows, heads, head_dim, the tables' widths), not by lengths.
+ * The same call gives the same bits each time; rows do not affect each other.
+ */
+as_status as_attend(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
+                    int64_t rows, const void *q, int64_t ldq, int32_t heads, float scale,
+                    int32_t window, int32_t sinks, void *out, int64_t ldo);
+
+/*
+ * The same for ragged queries: row r has offsets[r] .. offsets[r+1], those of its
+ * last tokens (all, or a chunk behind earlier ones), each of which sees the tokens
+ * up to its own.  Sequences without prompt_table (AS_ERR_UNSUPPORTED with one).
+ *   q, out     DEVICE [tokens, heads, head_dim], as in as_attend
+ *   tokens, offsets   as in as_cache_add, offsets not NULL; rows of out that are no
+ *              row's are not written
+ * A workspace as as_attend's, by tokens in place of rows, where there are few.
+ */
+as_status as_attend_prompts(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
+                            int64_t rows, const void *q, int64_t ldq, int64_t tokens,
+                            const int64_t *offsets, int32_t heads, float scale,
+                            int32_t window, int32_t sinks, void *out, int64_t ldo);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,6 +7,7 @@ that the seeded input generators (`synth`) stay importable on their own.
 _BINDING_NAMES = ("Ctx", "Model", "as_step", "as_step_ex", "as_lattice", "as_bigram_logits", "as_decode",
                   "as_interval_step", "as_encode", "as_decode_ancestral", "as_estimate_mean", "as_decode_fused", "as_bigram_group_mass", "as_step_fused",
                   "Layer", "Shaping", "as_linear", "as_shape_logits", "as_history_set", "as_history_add",
+                  "Cache", "Sequences", "as_cache_add", "as_attend", "as_attend_prompts",
                   "ArithSamplingError", "lib", "LIB_PATH", "AS_F32", "AS_BF16")
 
 

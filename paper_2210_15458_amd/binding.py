@@ -29,6 +29,18 @@ class _Shaping(C.Structure):
                 ("finished", C.c_void_p)]
 
 
+class _Cache(C.Structure):
+    """as_cache."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_int64), ("page_ld", C.c_int64), ("page_size", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int)]
+
+
+class _Sequences(C.Structure):
+    """as_sequences."""
+    _fields_ = [("table", C.c_void_p), ("table_ld", C.c_int64), ("lens", C.c_void_p), ("prompt_table", C.c_void_p),
+                ("prompt_table_ld", C.c_int64), ("prompt_lens", C.c_void_p), ("rows_per_prompt", C.c_int32), ("finished", C.c_void_p)]
+
+
 class ArithSamplingError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{_STATUS.get(code, code)}: {msg}")
@@ -72,6 +84,10 @@ def lib():
     L.as_linear.argtypes = [vp, vp, vp, i64, i64, vp, i64, shaping, vp, i64, C.c_int]
     L.as_history_set.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp, vp, i64, i32, vp, i64, i32, vp]
     L.as_history_add.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp]
+    cache, sequences = C.POINTER(_Cache), C.POINTER(_Sequences)
+    L.as_cache_add.argtypes = [vp, cache, sequences, i64, vp, i64, vp, i64, i64, vp]
+    L.as_attend.argtypes = [vp, cache, sequences, i64, vp, i64, i32, f32, i32, i32, vp, i64]
+    L.as_attend_prompts.argtypes = [vp, cache, sequences, i64, vp, i64, i64, vp, i32, f32, i32, i32, vp, i64]
     L.as_ctx_set_tuning.argtypes = [vp, C.c_int, i32]
     L.as_ctx_set_tuning.restype = C.c_int
     L.as_ctx_profile.argtypes = [vp, C.c_int]
@@ -84,7 +100,7 @@ def lib():
                  "as_model_create_bigram", "as_model_destroy", "as_bigram_logits", "as_decode",
                  "as_interval_step", "as_encode", "as_decode_ancestral", "as_estimate_mean", "as_decode_fused",
                  "as_bigram_group_mass", "as_step_fused", "as_shape_logits", "as_layer_create", "as_layer_destroy",
-                 "as_linear", "as_history_set", "as_history_add"):
+                 "as_linear", "as_history_set", "as_history_add", "as_cache_add", "as_attend", "as_attend_prompts"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -464,3 +480,116 @@ def as_history_add(ctx, seen, counts, tokens, finished=None):
     cp, cld = (None, 0) if counts is None else _rows(counts, torch.int32, "counts", rows, ctx.V)
     ctx._check(lib().as_history_add(ctx._h, sp, sld, cp, cld, rows, _dev(tokens, torch.int32, "tokens", rows),
                                     _dev(finished, torch.uint8, "finished", rows)))
+
+
+# ------------------------------------------------------------------------------- a cache and the attention that reads it
+
+class Cache:
+    """as_cache: keys and values [pages, kv_heads, page_size, head_dim], of one shape and dtype.  Borrowed: kept alive, and
+    written to by as_cache_add.  Each page is contiguous; the pages may be further apart (one layer's part of a larger tensor)."""
+
+    def __init__(self, k, v):
+        for name, t in (("k", k), ("v", v)):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a GPU tensor")
+            if t.dim() != 4:
+                raise ValueError(f"{name} must be [pages, kv_heads, page_size, head_dim]")
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride() != k.stride():
+            raise ValueError("k and v must have one shape, dtype, device and layout")
+        pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        page = self.kv_heads * self.page_size * self.head_dim
+        if pages and (not k[0].is_contiguous() or (pages > 1 and k.stride(0) < page)):
+            raise ValueError("the pages of k and v must be contiguous, one behind the other")
+        self.torch_dtype, self.device = k.dtype, k.device
+        self._tensors = (k, v)
+        c = self._c = _Cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else page, self.page_size, self.kv_heads, self.head_dim,
+                             _dtype_code(k))
+        self._ref = C.byref(c)
+
+
+class Sequences:
+    """as_sequences for `rows` rows: checked once, and the tensors kept alive; their contents may change from call to call."""
+
+    def __init__(self, rows, table=None, lens=None, prompt_table=None, prompt_lens=None, rows_per_prompt=1, finished=None):
+        self.rows = int(rows)
+        self._tensors = (table, lens, prompt_table, prompt_lens, finished)
+        devices = {t.device for t in self._tensors if t is not None}
+        if len(devices) > 1:
+            raise ValueError("the sequences' tensors must be on one device")
+        self.device = devices.pop() if devices else None
+        c = self._c = _Sequences()
+        if (table is None) != (lens is None) or (prompt_table is None) != (prompt_lens is None):
+            raise ValueError("a table needs its lengths, and lengths a table")
+        if table is not None:
+            c.table, c.table_ld = self._table(table, "table", self.rows)
+            c.lens = _dev(lens, torch.int32, "lens", self.rows)
+        if prompt_table is not None:
+            per = c.rows_per_prompt = int(rows_per_prompt)
+            if per < 1:
+                raise ValueError("rows_per_prompt must be at least 1")
+            prompts = -(-self.rows // per)
+            c.prompt_table, c.prompt_table_ld = self._table(prompt_table, "prompt_table", prompts)
+            c.prompt_lens = _dev(prompt_lens, torch.int32, "prompt_lens", prompts)
+        c.finished = _dev(finished, torch.uint8, "finished", self.rows)
+        self._ref = C.byref(c)
+
+    @staticmethod
+    def _table(t, name, rows):
+        ptr, ld = _rows(t, torch.int32, name, rows, 1)
+        if t.size(1) != ld:
+            raise ValueError(f"{name} must be contiguous")      # (its stride is how many pages a row may name)
+        return ptr, ld
+
+
+def _tokens_of(ctx, cache, seqs, t, dtype, name, rows, cols):
+    if isinstance(t, torch.Tensor) and t.dim() == 3 and t.stride(2) == 1 and (t.size(1) < 2 or t.stride(1) == t.size(2)):
+        t = t.as_strided((t.size(0), t.size(1) * t.size(2)), (t.stride(0), 1))
+    got = _rows(t, dtype, name, rows, cols)
+    if t.device != cache.device or (seqs.device is not None and seqs.device != cache.device) or ctx.stream.device != cache.device:
+        raise ValueError(f"{name}, the cache, the sequences and the context must be on one device")
+    return got
+
+
+def _offsets_of(cache, seqs, offsets):
+    if offsets.device != cache.device:
+        raise ValueError("offsets must be on the cache's device")
+    return _dev(offsets, torch.int64, "offsets", seqs.rows + 1)
+
+
+def as_cache_add(ctx, cache, seqs, k, v, offsets=None):
+    """Keys and values [tokens, kv_heads * head_dim] (or [tokens, kv_heads, head_dim]) of the rows' last tokens into their pages:
+    one a row, or with offsets [rows + 1] as many as they say."""
+    n, dtype, cols = k.size(0), cache.torch_dtype, cache.kv_heads * cache.head_dim
+    if offsets is None and n < seqs.rows:
+        raise ValueError(f"k has {n} rows, needs {seqs.rows}")
+    n = seqs.rows if offsets is None else n
+    kp, ldk = _tokens_of(ctx, cache, seqs, k, dtype, "k", n, cols)
+    vp, ldv = _tokens_of(ctx, cache, seqs, v, dtype, "v", n, cols)
+    ctx._check(lib().as_cache_add(ctx._h, cache._ref, seqs._ref, seqs.rows, kp, ldk, vp, ldv, n, None if offsets is None else _offsets_of(cache, seqs, offsets)))
+
+
+def _heads_of(cache, q):
+    cols = q.size(1) if q.dim() == 2 else q.size(1) * q.size(2)
+    if cols % cache.head_dim:
+        raise ValueError(f"q has {cols} columns, no whole number of heads of {cache.head_dim}")
+    return cols // cache.head_dim
+
+
+def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
+    """Attention of one query a row, q and out [rows, heads * head_dim] (or [rows, heads, head_dim]); scale: 1 / sqrt(head_dim)."""
+    heads, rows = _heads_of(cache, q), seqs.rows
+    qp, ldq = _tokens_of(ctx, cache, seqs, q, cache.torch_dtype, "q", rows, heads * cache.head_dim)
+    op, ldo = _tokens_of(ctx, cache, seqs, out, cache.torch_dtype, "out", rows, heads * cache.head_dim)
+    rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.head_dim ** -0.5 if scale is None else float(scale),
+                                   int(window), int(sinks), op, ldo)
+    if rc:
+        ctx._check(rc)
+
+
+def as_attend_prompts(ctx, cache, seqs, q, offsets, out, scale=None, window=0, sinks=0):
+    """The same for ragged queries: row r has q[offsets[r]:offsets[r + 1]], those of its last tokens."""
+    heads, n = _heads_of(cache, q), q.size(0)
+    qp, ldq = _tokens_of(ctx, cache, seqs, q, cache.torch_dtype, "q", n, heads * cache.head_dim)
+    op, ldo = _tokens_of(ctx, cache, seqs, out, cache.torch_dtype, "out", n, heads * cache.head_dim)
+    ctx._check(lib().as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, _offsets_of(cache, seqs, offsets), heads,
+                                       cache.head_dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), op, ldo))

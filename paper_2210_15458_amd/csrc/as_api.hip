@@ -284,6 +284,7 @@ as_status as_ctx_destroy(as_ctx *ctx)
     if (ctx->encode_logits.ptr) (void)hipFree(ctx->encode_logits.ptr);
     if (ctx->encode_state.ptr) (void)hipFree(ctx->encode_state.ptr);
     if (ctx->linear_x.ptr) (void)hipFree(ctx->linear_x.ptr);
+    if (ctx->attend_parts.ptr) (void)hipFree(ctx->attend_parts.ptr);
     for (auto &v : ctx->prof.slots)
         for (auto &s : v) {
             (void)hipEventDestroy(s.start);
@@ -1234,6 +1235,121 @@ as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
     HistoryArgs a{};
     a.seen = seen; a.seen_ld = seen_ld; a.counts = counts; a.counts_ld = counts_ld; a.rows = rows; a.V = ctx->V;
     return launch_history_add(ctx, a, tokens, finished);
+}
+
+// A cache and the sequences in it, as the kernels take them.
+static as_status check_cache(as_ctx *ctx, const as_cache *c, const as_sequences *s, int64_t rows, AttendArgs *a)
+{
+    if (!c || !s) return fail(ctx, AS_ERR_INVALID_ARG, "cache and sequences must not be NULL");
+    if (rows < 0 || rows > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "rows outside [0, max_rows]");
+    if (!c->k || !c->v) return fail(ctx, AS_ERR_INVALID_ARG, "the cache's k and v must not be NULL");
+    if (c->dtype != AS_F32 && c->dtype != AS_BF16) return fail(ctx, AS_ERR_INVALID_ARG, "unknown cache dtype");
+    if (c->pages < 1 || c->pages > 0x7fffffffLL) return fail(ctx, AS_ERR_INVALID_ARG, "pages outside [1, 2^31)");
+    if (c->page_size < 1 || c->page_size > AS_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0)
+        return fail(ctx, AS_ERR_INVALID_ARG, "page_size must be a power of two of at most AS_MAX_PAGE");
+    if (c->head_dim < 8 || c->head_dim > AS_MAX_HEAD_DIM || c->head_dim % 8 != 0)
+        return fail(ctx, AS_ERR_INVALID_ARG, "head_dim must be a multiple of 8 in [8, AS_MAX_HEAD_DIM]");
+    if (c->kv_heads < 1 || c->kv_heads > AS_MAX_HEADS) return fail(ctx, AS_ERR_INVALID_ARG, "kv_heads outside [1, AS_MAX_HEADS]");
+    const int64_t esz = c->dtype == AS_BF16 ? 2 : 4, page = (int64_t)c->kv_heads * c->page_size * c->head_dim;
+    if (c->page_ld < page || c->page_ld > (int64_t)1 << 40) return fail(ctx, AS_ERR_INVALID_ARG, "page_ld is smaller than a page, or larger than 2^40");
+    if (!all_aligned(16, {c->k, c->v}) || c->page_ld * esz % 16 != 0)
+        return fail(ctx, AS_ERR_INVALID_ARG, "k, v and their pages must lie on 16 bytes");
+    if (s->table && (!s->lens || s->table_ld < 1)) return fail(ctx, AS_ERR_INVALID_ARG, "table needs lens and table_ld >= 1");
+    if (s->prompt_table && (!s->prompt_lens || s->prompt_table_ld < 1 || s->rows_per_prompt < 1))
+        return fail(ctx, AS_ERR_INVALID_ARG, "prompt_table needs prompt_lens, prompt_table_ld >= 1 and rows_per_prompt >= 1");
+    const int64_t most = (int64_t)1 << 30;
+    if ((s->table && s->table_ld > most / c->page_size) || (s->prompt_table && s->prompt_table_ld > most / c->page_size))
+        return fail(ctx, AS_ERR_INVALID_ARG, "a table of more than 2^30 tokens");
+    if (!all_aligned(4, {s->table, s->prompt_table}) || !all_aligned(4, {s->table ? s->lens : nullptr, s->prompt_table ? s->prompt_lens : nullptr}))
+        return fail(ctx, AS_ERR_INVALID_ARG, "table, lens, prompt_table or prompt_lens is not aligned to its element type");
+    *a = AttendArgs{};
+    a->k = c->k; a->v = c->v; a->pages = c->pages; a->page_bytes = c->page_ld * esz; a->kv_heads = c->kv_heads; a->dim = c->head_dim;
+    a->dtype = c->dtype;
+    while ((1 << a->page_shift) < c->page_size) ++a->page_shift;
+    a->rows = rows; a->tokens = rows; a->finished = s->finished;
+    if (s->table) {
+        a->table = s->table; a->table_ld = s->table_ld; a->lens = s->lens; a->room = (int32_t)(s->table_ld * c->page_size);
+    }
+    a->per = 1;
+    if (s->prompt_table) {
+        a->prompt_table = s->prompt_table; a->prompt_table_ld = s->prompt_table_ld; a->prompt_lens = s->prompt_lens;
+        a->prompt_room = (int32_t)(s->prompt_table_ld * c->page_size);
+        a->per = s->rows_per_prompt < rows || rows == 0 ? s->rows_per_prompt : (int32_t)rows;
+    }
+    return AS_OK;
+}
+
+static as_status check_queries(as_ctx *ctx, AttendArgs *a, const void *q, int64_t ldq, int32_t heads, float scale, int32_t window, int32_t sinks,
+                               void *out, int64_t ldo)
+{
+    if (heads < 1 || heads > AS_MAX_HEADS || heads % a->kv_heads != 0)
+        return fail(ctx, AS_ERR_INVALID_ARG, "heads must be a multiple of kv_heads in [1, AS_MAX_HEADS]");
+    if (!isfinite(scale)) return fail(ctx, AS_ERR_INVALID_ARG, "scale must be finite");
+    if (sinks < 0) return fail(ctx, AS_ERR_INVALID_ARG, "sinks is negative");
+    if (a->tokens == 0) return AS_OK;
+    if (!q || !out) return fail(ctx, AS_ERR_INVALID_ARG, "q and out must not be NULL");
+    if (ldq < (int64_t)heads * a->dim || ldo < (int64_t)heads * a->dim) return fail(ctx, AS_ERR_INVALID_ARG, "ldq or ldo is smaller than its rows");
+    if (!aligned_to(q, a->dtype) || !aligned_to(out, a->dtype)) return fail(ctx, AS_ERR_INVALID_ARG, "q or out is not aligned to its element type");
+    a->q = q; a->ldq = ldq; a->out = out; a->ldo = ldo; a->heads = heads; a->group = heads / a->kv_heads;
+    a->scale = scale * 1.44269504088896340736f;
+    a->window = window > 0 ? window : 0;
+    a->sinks = sinks;
+    return AS_OK;
+}
+
+as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences, int64_t rows, const void *k, int64_t ldk, const void *v,
+                       int64_t ldv, int64_t tokens, const int64_t *offsets)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    AttendArgs a;
+    const as_status st = check_cache(ctx, cache, sequences, rows, &a);
+    if (st != AS_OK) return st;
+    if (!a.table) return fail(ctx, AS_ERR_INVALID_ARG, "new tokens need a table");
+    if (tokens < 0 || tokens > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "tokens outside [0, max_rows]");
+    if (!offsets && tokens != rows) return fail(ctx, AS_ERR_INVALID_ARG, "without offsets there is a token a row");
+    if (!all_aligned(8, {offsets})) return fail(ctx, AS_ERR_INVALID_ARG, "offsets is not aligned to its element type");
+    if (tokens == 0 || rows == 0) return AS_OK;
+    if (!k || !v) return fail(ctx, AS_ERR_INVALID_ARG, "k and v must not be NULL");
+    if (ldk < (int64_t)a.kv_heads * a.dim || ldv < (int64_t)a.kv_heads * a.dim)
+        return fail(ctx, AS_ERR_INVALID_ARG, "ldk or ldv is smaller than its rows");
+    if (!aligned_to(k, a.dtype) || !aligned_to(v, a.dtype)) return fail(ctx, AS_ERR_INVALID_ARG, "k or v is not aligned to its element type");
+    a.tokens = tokens;
+    a.offsets = offsets;
+    return launch_cache_add(ctx, a, k, ldk, v, ldv);
+}
+
+as_status as_attend(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences, int64_t rows, const void *q, int64_t ldq, int32_t heads,
+                    float scale, int32_t window, int32_t sinks, void *out, int64_t ldo)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    AttendArgs a;
+    as_status st = check_cache(ctx, cache, sequences, rows, &a);
+    if (st == AS_OK && !a.table && !a.prompt_table) st = fail(ctx, AS_ERR_INVALID_ARG, "sequences without table and prompt_table");
+    if (st == AS_OK) st = check_queries(ctx, &a, q, ldq, heads, scale, window, sinks, out, ldo);
+    if (st != AS_OK || rows == 0) return st;
+    st = grow(ctx, ctx->attend_parts, attend_workspace(ctx, a));
+    return st == AS_OK ? launch_attend(ctx, a) : st;
+}
+
+as_status as_attend_prompts(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences, int64_t rows, const void *q, int64_t ldq,
+                            int64_t tokens, const int64_t *offsets, int32_t heads, float scale, int32_t window, int32_t sinks, void *out,
+                            int64_t ldo)
+{
+    if (!ctx) return fail(nullptr, AS_ERR_INVALID_ARG, "ctx is NULL");
+    AttendArgs a;
+    as_status st = check_cache(ctx, cache, sequences, rows, &a);
+    if (st != AS_OK) return st;
+    if (a.prompt_table) return fail(ctx, AS_ERR_UNSUPPORTED, "prompts have pages of their own: no prompt_table");
+    if (!a.table) return fail(ctx, AS_ERR_INVALID_ARG, "prompts need a table");
+    if (tokens < 0 || tokens > ctx->max_rows) return fail(ctx, AS_ERR_INVALID_ARG, "tokens outside [0, max_rows]");
+    if (!offsets) return fail(ctx, AS_ERR_INVALID_ARG, "offsets must not be NULL");
+    if (!all_aligned(8, {offsets})) return fail(ctx, AS_ERR_INVALID_ARG, "offsets is not aligned to its element type");
+    a.tokens = tokens;
+    a.offsets = offsets;
+    st = check_queries(ctx, &a, q, ldq, heads, scale, window, sinks, out, ldo);
+    if (st != AS_OK || rows == 0 || tokens == 0) return st;
+    st = grow(ctx, ctx->attend_parts, attend_workspace(ctx, a));
+    return st == AS_OK ? launch_attend(ctx, a) : st;
 }
 
 }  // extern "C"

@@ -1,0 +1,682 @@
+// A paged cache of keys and values, and the attention that reads it.
+//
+// Row r's query at position i over keys j:  s_j = scale q.k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  m = max_j s_j, over
+// the j that it sees (j <= i; with a window j > i - window or j < sinks).  Keys are taken a tile at a time, with the running m,
+// l = sum exp(s_j - m) and O = sum exp(s_j - m) v_j; a tile that raises m by d multiplies l and O by exp(-d).  Parts of the keys that
+// different waves or blocks have taken are joined the same way:  m = max m_a, l = sum l_a exp(m_a - m), O = sum O_a exp(m_a - m).
+#include <type_traits>
+
+#include "as_shape.hpp"
+
+namespace as {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+constexpr float kNone = -__builtin_inff();
+
+// ---------------------------------------------------------------- which queries, which keys
+
+// Ragged queries go by tiles of `rows` rows (a row: one head of those that share a key head, of one token); sequence s has the
+// slots floor(offsets[s] * group / rows) + s on, one a tile: never fewer than its tiles, and in order, so a block finds
+// its sequence by a search in the offsets alone.
+__device__ __forceinline__ int64_t offset_at(const AttendArgs &a, int64_t s)
+{
+    const int64_t o = a.offsets[s];
+    return o < 0 ? 0 : o > a.tokens ? a.tokens : o;
+}
+// The last sequence whose first slot is at most `slot` (rows 0: whose first token is); 64 of them looked at at once.
+__device__ __forceinline__ int64_t find_sequence(const AttendArgs &a, int64_t slot, int32_t group, int32_t rows)
+{
+    int64_t lo = 0, hi = a.rows;                       // the answer is in [lo, hi)
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, s = lo + (lane_id() + 1) * step;
+        const bool behind = s < hi && (rows ? offset_at(a, s) * group / rows + s : offset_at(a, s)) <= slot;
+        const int n = __popcll(__ballot(behind));      // (monotone: the first n lanes)
+        const int64_t next = lo + n * step;
+        hi = next + step < hi ? next + step : hi;
+        lo = next;
+    }
+    return lo;
+}
+
+// What a block works on: up to `rows` queries that share a key head, and a segment of keys.
+struct Work {
+    int32_t head;                 // key head
+    const int32_t *table;         // the segment's pages
+    int32_t n;                    // its keys
+    int32_t key0;                 // position of its first key
+    // of a lane's query: whether there is one, its token and head, its position relative to the segment's first key
+    bool valid;
+    int64_t token;
+    int32_t qhead, at;
+};
+
+__device__ __forceinline__ int32_t length_of(const int32_t *lens, int64_t i, int32_t room)
+{
+    const int32_t n = scalar_load(lens + i);
+    return n < 0 ? 0 : n > room ? room : n;
+}
+
+// Query `mine` (0 .. rows-1) of tile blockIdx.x.  False where the block has nothing to do.
+__device__ __forceinline__ bool find_work(const AttendArgs &a, int32_t mode, int32_t rows, int32_t tiles, int32_t mine, int64_t item, Work &w)
+{
+    const int32_t G = a.group;
+    if (mode == kAttendRagged) {
+        const int64_t slot = item / a.kv_heads;
+        w.head = (int32_t)(item - slot * a.kv_heads);
+        const int64_t s = find_sequence(a, slot, G, rows);
+        const int64_t from = offset_at(a, s), to = offset_at(a, s + 1);
+        const int64_t first = (slot - s - from * G / rows) * rows;      // the tile's first row in its sequence
+        const int64_t all = (to - from) * G;
+        if (first < 0 || first >= all || (a.finished && a.finished[s])) return false;      // (below 0: offsets that fall)
+        const int32_t len = length_of(a.lens, s, a.room);
+        w.table = a.table + s * a.table_ld;
+        w.n = len;
+        w.key0 = 0;
+        const int64_t m = first + mine;
+        w.valid = m < all;
+        const int32_t i = (int32_t)((w.valid ? m : all - 1) / G);
+        w.token = from + i;
+        w.qhead = w.head * G + (int32_t)(m - (int64_t)i * G);
+        w.at = len - (int32_t)(to - from) + i;
+        return true;
+    }
+    const int32_t tile = (int32_t)(item % tiles);
+    const int64_t rest = item / tiles;
+    w.head = (int32_t)(rest % a.kv_heads);
+    const int64_t p = rest / a.kv_heads;                // row or prompt
+    if (mode == kAttendOwn) {
+        if (a.finished && a.finished[p]) return false;
+        const int32_t g = tile * rows + mine;
+        w.valid = g < G;
+        w.token = p;
+        w.qhead = w.head * G + g;
+        w.table = a.table + p * a.table_ld;
+        w.n = length_of(a.lens, p, a.room);
+        w.key0 = a.prompt_table ? length_of(a.prompt_lens, p / a.per, a.prompt_room) : 0;
+        w.at = w.n - 1;
+        return true;
+    }
+    w.table = a.prompt_table + p * a.prompt_table_ld;
+    w.n = length_of(a.prompt_lens, p, a.prompt_room);
+    w.key0 = 0;
+    const int64_t m = (int64_t)tile * rows + mine;
+    const int64_t c = m / G, row = p * a.per + c;
+    w.valid = c < a.per && row < a.rows;
+    if (w.valid && a.finished && a.finished[row]) w.valid = false;
+    w.token = row;
+    w.qhead = w.head * G + (int32_t)(m - c * G);
+    int32_t own = 0;
+    if (w.valid && a.table) {
+        own = a.lens[row];
+        own = own < 0 ? 0 : own > a.room ? a.room : own;
+    }
+    w.at = w.n + own - 1;
+    return true;
+}
+
+// The tiles of BN keys that some query of a block may see, and this part's share of them.
+struct Keys {
+    int32_t n, lo_at, hi_at;      // keys; smallest and largest position of the queries
+    int32_t lo, hi;               // the keys seen by some query: [lo, hi) and [0, sinks)
+    int32_t window, sinks;
+    int32_t sink_tiles, main_tile, first, last;
+    __device__ __forceinline__ int32_t base(int32_t t, int32_t BN) const { return (t < sink_tiles ? t : t - sink_tiles + main_tile) * BN; }
+    // every query sees every key of the tile
+    __device__ __forceinline__ bool whole(int32_t b, int32_t BN) const
+    {
+        return b + BN <= n && b + BN - 1 <= lo_at && (window <= 0 || b > hi_at - window || b + BN <= sinks);
+    }
+    __device__ __forceinline__ bool seen(int32_t t, int32_t at) const
+    {
+        return t < n && t <= at && (window <= 0 || t > at - window || t < sinks);
+    }
+    __device__ __forceinline__ bool seen_by_some(int32_t t) const { return t < hi && (t >= lo || t < sinks); }
+};
+
+__device__ __forceinline__ Keys keys_of(const AttendArgs &a, const Work &w, int32_t lo_at, int32_t hi_at, int32_t BN, int32_t part, int32_t parts,
+                                        int32_t least)
+{
+    Keys k;
+    k.n = w.n;
+    k.lo_at = lo_at;
+    k.hi_at = hi_at;
+    k.window = a.window;
+    k.sinks = a.sinks - w.key0;
+    k.hi = w.n < hi_at + 1 ? w.n : hi_at + 1;
+    k.hi = k.hi > 0 ? k.hi : 0;
+    k.lo = a.window > 0 && lo_at - a.window + 1 > 0 ? lo_at - a.window + 1 : 0;
+    k.lo = k.lo < k.hi ? k.lo : k.hi;
+    const int32_t first = k.sinks < 0 ? 0 : k.sinks < k.lo ? k.sinks : k.lo;
+    k.sink_tiles = (first + BN - 1) / BN;
+    k.main_tile = k.lo / BN;
+    if (k.sink_tiles >= k.main_tile) k.sink_tiles = k.main_tile = 0;
+    const int32_t count = k.sink_tiles + (k.hi + BN - 1) / BN - k.main_tile;
+    int32_t share = (count + parts - 1) / parts;
+    share = share > least ? share : least;
+    k.first = part * share < count ? part * share : count;
+    k.last = count - k.first < share ? count : k.first + share;
+    return k;
+}
+
+// Address of a key head's token t.
+__device__ __forceinline__ const char *token_at(const void *cache, const AttendArgs &a, const Work &w, int32_t t, int32_t esz)
+{
+    int32_t page = w.table[t >> a.page_shift];
+    page = page < 0 ? 0 : page < a.pages ? page : (int32_t)a.pages - 1;
+    return (const char *)cache + (int64_t)page * a.page_bytes +
+           (((int64_t)w.head << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * (int64_t)(a.dim * esz);
+}
+
+// The words' values that are no numbers (infinities, NaN): whether there are any, from the largest magnitudes; and the words without.
+template <class T> __device__ __forceinline__ uint32_t larger_magnitude(uint32_t a, uint32_t x)
+{
+    if constexpr (sizeof(T) == 2) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+    } else {
+        x &= 0x7fffffffu;
+        return a > x ? a : x;
+    }
+}
+template <class T> __device__ __forceinline__ bool no_number(uint32_t a)
+{
+    return a >= 0x7f800000u || (sizeof(T) == 2 && (a & 0xffffu) >= 0x7f80u);
+}
+template <class T> __device__ __forceinline__ uint32_t numbers(uint32_t x)
+{
+    const uint32_t high = (x & 0x7f800000u) == 0x7f800000u ? 0u : sizeof(T) == 2 ? x & 0xffff0000u : x;
+    return sizeof(T) == 2 ? high | ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) : high;
+}
+
+// What a wave left out of its product: the values that are no numbers in the tiles that not every query sees whole, to the sums of
+// those that do see them (0 * NaN is NaN, so the product cannot leave them out by their weight).
+template <class T, int QUERIES, int EVERY>
+__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Work &w, const Keys &keys, int32_t BN, int32_t from, int32_t at,
+                                                         float *sums, int32_t stride)
+{
+    for (int32_t t = keys.first + from; t < keys.last; t += EVERY) {
+        const int32_t base = keys.base(t, BN);
+        if (keys.whole(base, BN)) continue;
+        for (int32_t x = base; x < base + BN && x < keys.hi; ++x) {
+            if (!keys.seen_by_some(x)) continue;
+            const T *const row = (const T *)token_at(a.v, a, w, x, sizeof(T));
+            for (int32_t d = lane_id(); d - lane_id() < a.dim; d += kWave) {
+                const float y = d < a.dim ? widen(row[d]) : 0.f;
+                const bool is = (__builtin_bit_cast(uint32_t, y) & 0x7f800000u) == 0x7f800000u;
+                if (!__any(is)) continue;
+                for (int q = 0; q < QUERIES; ++q)
+                    if (keys.seen(x, __builtin_amdgcn_readlane(at, q)) && is) sums[q * stride + d] += y;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- 16 queries a block, keys straight from memory
+
+// A wave takes tiles of keys from memory to registers, 16 queries at a time (of one key head: the heads of a row that share it, or
+// rows of a prompt, or tokens of a sequence), the four waves of a block every fourth tile, joined at the end.  Both products are
+// taken transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane's scores, its share of P^T and its sums all are of one query
+// (lane % 16), whose m and l it carries.  A lane of quarter q = lane / 16 gets from the first product the scores of tokens
+// 16 a + 4 q + j (a: 16 tokens of the tile, j < 4), and hands them to the second as its share of the sum over tokens, which may go
+// in any order as long as V^T's lanes have the same tokens: so V is read in whole rows, 16 lanes one token, and the 2-byte
+// values of a lane's tokens are put in pairs by byte permutations, without LDS.
+template <class T, int DP> struct AttendForm;
+template <int DP> struct AttendForm<uint16_t, DP> {
+    static constexpr int kSub = 2, kKey = DP / 32, kVBytes = DP == 64 ? 8 : 16, kChunks = DP == 256 ? 2 : 1, kEach = kVBytes / 2;
+};
+template <int DP> struct AttendForm<float, DP> {
+    static constexpr int kSub = 1, kKey = DP / 16, kVBytes = 16, kChunks = DP / 64, kEach = 4;
+};
+
+template <class T, int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPiece piece)
+{
+    typedef AttendForm<T, DP> F;
+    constexpr int kSub = F::kSub, kKey = F::kKey, kVBytes = F::kVBytes, kChunks = F::kChunks, kEach = F::kEach, BN = 16 * kSub;
+    constexpr int kStride = DP + 4, kWords = kVBytes / 4;
+    constexpr bool kBf16 = sizeof(T) == 2;
+    __shared__ __attribute__((aligned(16))) float sums[4 * 16 * kStride];
+    __shared__ float2 stats[4][16];
+    __shared__ int64_t rows_at[16];                    // token * heads + head of each query, -1: none
+    const int lane = threadIdx.x & 63, quarter = lane >> 4, mine = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t bytes = a.dim * (int32_t)sizeof(T);
+    Work w;
+    if (!find_work(a, piece.mode, 16, piece.tiles, mine, blockIdx.x, w)) return;
+    int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = w.valid ? w.at : -1;
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        const int32_t u = __shfl_xor(lo_at, d, kWave), v = __shfl_xor(hi_at, d, kWave);
+        lo_at = u < lo_at ? u : lo_at;
+        hi_at = v > hi_at ? v : hi_at;
+    }
+    lo_at = __builtin_amdgcn_readfirstlane(lo_at);
+    hi_at = __builtin_amdgcn_readfirstlane(hi_at);
+    if (lo_at > hi_at) lo_at = hi_at;                  // (no query)
+    const Keys keys = keys_of(a, w, lo_at, hi_at, BN, blockIdx.y, piece.parts, piece.least);
+    const int32_t at = w.valid ? w.at : -1;
+
+    // the queries, zeros where there is none and past the row's end
+    u32x4 q[kKey];
+    {
+        const char *const from = (const char *)a.q + (w.token * a.ldq + (int64_t)w.qhead * a.dim) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kKey; ++i) {
+            const int32_t o = (i * 4 + quarter) * 16;
+            q[i] = u32x4{0, 0, 0, 0};
+            if (w.valid && (FULL || o < bytes)) q[i] = *reinterpret_cast<const u32x4_any *>(from + o);
+        }
+    }
+    f32x4 o[kChunks][kEach];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) o[c][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kNone, l = 0.f;
+    bool odd = false;
+
+#pragma unroll 1
+    for (int32_t t = keys.first + wave; t < keys.last; t += 4) {
+        const int32_t base = keys.base(t, BN);
+        u32x4 k[kSub][kKey];
+        uint32_t v[kSub * 4][kChunks][kWords];
+        const char *kp[kSub], *vp[kSub];
+        if constexpr (BYPAGE) {
+            // 16 tokens lie in one page
+#pragma unroll
+            for (int s = 0; s < kSub; ++s) {
+                const int32_t first = base + 16 * s, there = first < keys.n ? first : base;
+                int32_t page = scalar_load(w.table + (there >> a.page_shift));
+                page = page < 0 ? 0 : page < a.pages ? page : (int32_t)a.pages - 1;
+                const int64_t off = (int64_t)page * a.page_bytes +
+                                    (((int64_t)w.head << a.page_shift) + (there & ((1 << a.page_shift) - 1))) * (int64_t)bytes;
+                kp[s] = (const char *)a.k + off;
+                vp[s] = (const char *)a.v + off;
+            }
+        }
+        auto key_row = [&](int s) __attribute__((always_inline)) -> const char * {
+            if constexpr (BYPAGE) return kp[s] + mine * bytes;
+            const int32_t x = base + 16 * s + mine;
+            return token_at(a.k, a, w, x < keys.n ? x : keys.n - 1, sizeof(T));
+        };
+        auto value_row = [&](int e) __attribute__((always_inline)) -> const char * {
+            if constexpr (BYPAGE) return vp[e >> 2] + (quarter * 4 + (e & 3)) * bytes;
+            const int32_t x = base + 16 * (e >> 2) + quarter * 4 + (e & 3);
+            return token_at(a.v, a, w, x < keys.n ? x : keys.n - 1, sizeof(T));
+        };
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) {
+            const char *const row = key_row(s);
+#pragma unroll
+            for (int i = 0; i < kKey; ++i) {
+                const int32_t at_byte = (i * 4 + quarter) * 16;
+                if (FULL) k[s][i] = *reinterpret_cast<const u32x4 *>(row + at_byte);
+                else {
+                    k[s][i] = *reinterpret_cast<const u32x4 *>(row + (at_byte < bytes ? at_byte : 0));
+                    if (at_byte >= bytes) k[s][i] = u32x4{0, 0, 0, 0};
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kSub * 4; ++e) {
+            const char *const row = value_row(e);
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const int32_t at_byte = (c * 16 + mine) * kVBytes;
+                const char *const p = row + (FULL || at_byte < bytes ? at_byte : 0);
+                if constexpr (kVBytes == 8) {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+                    v[e][c][0] = x[0];
+                    v[e][c][1] = x[1];
+                } else {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[e][c][i] = x[i];
+                }
+                if (!FULL && at_byte >= bytes) {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) v[e][c][i] = 0;
+                }
+            }
+        }
+        // scores
+        f32x4 s4[kSub];
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) {
+            s4[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kKey; ++i) {
+                if constexpr (kBf16) {
+                    s4[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[s][i]), __builtin_bit_cast(bf16x8, q[i]), s4[s], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s4[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[s][i][e]),
+                                                                     __builtin_bit_cast(float, (uint32_t)q[i][e]), s4[s], 0, 0, 0);
+                }
+            }
+        }
+        float p[kSub * 4];
+#pragma unroll
+        for (int e = 0; e < kSub * 4; ++e) p[e] = s4[e >> 2][e & 3] * a.scale;
+        if (!keys.whole(base, BN)) {
+            uint32_t largest = 0;
+#pragma unroll
+            for (int e = 0; e < kSub * 4; ++e) {
+                const int32_t x = base + 16 * (e >> 2) + quarter * 4 + (e & 3);
+                p[e] = keys.seen(x, at) ? p[e] : kNone;
+                // what no query sees may be anything, and 0 * NaN is NaN
+                const uint32_t keep = keys.seen_by_some(x) ? 0xffffffffu : 0u;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        v[e][c][i] &= keep;
+                        largest = larger_magnitude<T>(largest, v[e][c][i]);
+                    }
+            }
+            // A value that is no number, seen by some queries and not by others of the tile: it is left out of the product, and
+            // added to those that see it at the end.
+            if (lo_at != hi_at && __any(no_number<T>(largest))) {
+                odd = true;
+#pragma unroll
+                for (int e = 0; e < kSub * 4; ++e)
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                        for (int i = 0; i < kWords; ++i) v[e][c][i] = numbers<T>(v[e][c][i]);
+            }
+        }
+        // the running maximum, the same in the four lanes of a query
+        float top = p[0];
+#pragma unroll
+        for (int e = 1; e < kSub * 4; ++e) top = fmaxf(top, p[e]);
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        if (__any(top > m)) {
+            const float now = fmaxf(top, m);
+            const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) o[c][e] *= by;
+        }
+        const float ref = m == kNone ? 0.f : m;
+#pragma unroll
+        for (int e = 0; e < kSub * 4; ++e) p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+        if constexpr (kBf16) {
+            // Weights go into the product as bf16; l adds up the rounded ones, so that they come to 1 all the same.
+            u32x4 pw;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                pw[i] = pack2_bf16(p[2 * i], p[2 * i + 1]);
+                l += __builtin_bit_cast(float, (uint32_t)pw[i] << 16) + __builtin_bit_cast(float, (uint32_t)pw[i] & 0xffff0000u);
+            }
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    u32x4 vw;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        vw[i] = __builtin_amdgcn_perm(v[2 * i + 1][c][e >> 1], v[2 * i][c][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+                    o[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vw), __builtin_bit_cast(bf16x8, pw), o[c][e], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                l += p[j];
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e)
+                        o[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[j][c][e]), p[j], o[c][e], 0, 0, 0);
+            }
+        }
+    }
+
+    // the four waves' parts
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (l != l && m == kNone) m = 0.f;                 // (a query that is no number: its maximum says nothing, its sum does)
+    if (quarter == 0) stats[wave][mine] = float2{m, l};
+    if (threadIdx.x < 16) rows_at[mine] = w.valid ? w.token * a.heads + w.qhead : -1;
+    __syncthreads();
+    float M = kNone;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, stats[i][mine].x);
+    const float by = m == kNone ? 0.f : __builtin_amdgcn_exp2f(m - M);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float *const to = sums + (wave * 16 + mine) * kStride + (c * 16 + quarter * 4 + r) * kEach;
+#pragma unroll
+            for (int e = 0; e < kEach; e += 4) {
+                f32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = o[c][e + i][r] * by;
+                *reinterpret_cast<f32x4 *>(to + e) = x;
+            }
+        }
+    if (odd) add_odd_values<T, 16, 4>(a, w, keys, BN, wave, at, sums + wave * 16 * kStride, kStride);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (DP / 8); i += 256) {
+        const int r = i / (DP / 8), d = i % (DP / 8) * 8;
+        if (d >= a.dim) continue;
+        const int64_t row = rows_at[r];
+        if (row < 0) continue;
+        float top = kNone, total = 0.f, y[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, stats[j][r].x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (stats[j][r].x != kNone) total += stats[j][r].y * __builtin_amdgcn_exp2f(stats[j][r].x - top);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += sums[(j * 16 + r) * kStride + d + e];
+        if (a.parts == 1) {
+            const float inverse = total > 0.f || total != total ? 1.f / total : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] *= inverse;
+            const int64_t token = row / a.heads;
+            store8((T *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
+        } else {
+            const int64_t at_part = row * a.parts + piece.part0 + blockIdx.y;
+            if (d == 0) a.stats[at_part] = float2{top, total};
+            if (top != kNone) store8(a.sums + at_part * a.dim + d, y);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- parts joined
+
+// A wave a query head: the parts' m and l a lane each, then their sums a part after the other.
+template <class T>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t token = i / a.heads;
+    if (token >= a.tokens) return;
+    if (a.offsets) {
+        if (token < offset_at(a, 0) || token >= offset_at(a, a.rows)) return;
+        if (a.finished && a.finished[find_sequence(a, token, 1, 0)]) return;
+    } else if (a.finished && a.finished[token]) return;
+    const float2 *const stats = a.stats + i * a.parts;
+    const float2 mine = lane < a.parts ? stats[lane] : float2{kNone, 0.f};
+    const float M = wave_max(mine.x);
+    const float weight = mine.x == kNone ? 0.f : __builtin_amdgcn_exp2f(mine.x - M);
+    const float total = wave_sum(weight * mine.y);
+    const float inverse = total > 0.f || total != total ? 1.f / total : 0.f;
+    const uint64_t there = __ballot(mine.x != kNone);
+    const float *const sums = a.sums + i * a.parts * a.dim;
+    T *const out = (T *)a.out + token * a.ldo + (i - token * a.heads) * a.dim;
+    for (int32_t d = lane * 8; d < a.dim; d += kWave * 8) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = 0.f;
+        for (uint64_t rest = there; rest; rest &= rest - 1) {
+            const int p = __builtin_ctzll(rest);
+            const float by = read_lane(weight, p);
+            Raw8<float> x;
+            load_raw8(sums + (int64_t)p * a.dim + d, x);
+            float z[8];
+            widen8(x, z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = fmaf(z[e], by, y[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= inverse;
+        store8(out + d, y);
+    }
+}
+
+template <class T, int DP>
+static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+{
+    if (a.page_shift < 4) hipLaunchKernelGGL((attend_rows_kernel<T, DP, false, false>), grid, dim3(256), 0, ctx->stream, a, p);
+    else if (a.dim != DP) hipLaunchKernelGGL((attend_rows_kernel<T, DP, false, true>), grid, dim3(256), 0, ctx->stream, a, p);
+    else hipLaunchKernelGGL((attend_rows_kernel<T, DP, true, true>), grid, dim3(256), 0, ctx->stream, a, p);
+}
+template <class T>
+static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+{
+    if (a.dim <= 64) rows_of<T, 64>(ctx, a, p, grid);
+    else if (a.dim <= 128) rows_of<T, 128>(ctx, a, p, grid);
+    else rows_of<T, 256>(ctx, a, p, grid);
+}
+
+// What a call comes to: the launches, and the parts that each leaves.
+struct AttendPlan {
+    AttendPiece piece[2];
+    int64_t blocks[2];
+    int count = 0;
+    int32_t parts = 0;
+};
+
+static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room)
+{
+    int64_t n = (2 * (int64_t)ctx->num_cus + blocks - 1) / blocks;
+    const int64_t most = (room + 255) / 256;
+    n = n < most ? n : most;
+    return (int32_t)(n < 1 ? 1 : n > kAttendMostParts ? kAttendMostParts : n);
+}
+
+static AttendPlan plan_of(const as_ctx *ctx, const AttendArgs &a)
+{
+    AttendPlan p;
+    auto add = [&](int mode, int64_t blocks, int32_t tiles, int64_t room) {
+        AttendPiece &x = p.piece[p.count];
+        x.mode = mode;
+        x.tiles = tiles;
+        x.least = 8;
+        x.part0 = p.parts;
+        x.parts = parts_for(ctx, blocks, room);
+        p.parts += x.parts;
+        p.blocks[p.count++] = blocks;
+    };
+    if (a.offsets) add(kAttendRagged, (a.tokens * a.group / 16 + a.rows) * a.kv_heads, 1, a.room);
+    else {
+        if (a.prompt_table) {
+            const int32_t tiles = (int32_t)((a.per * (int64_t)a.group + 15) / 16);
+            add(kAttendShared, (a.rows + a.per - 1) / a.per * a.kv_heads * tiles, tiles, a.prompt_room);
+        }
+        if (a.table) {
+            const int32_t tiles = (a.group + 15) / 16;
+            add(kAttendOwn, a.rows * a.kv_heads * tiles, tiles, a.room);
+        }
+    }
+    return p;
+}
+
+size_t attend_workspace(const as_ctx *ctx, const AttendArgs &a)
+{
+    const AttendPlan p = plan_of(ctx, a);
+    return p.parts < 2 ? 0 : (size_t)a.tokens * a.heads * p.parts * (sizeof(float2) + (size_t)a.dim * sizeof(float));
+}
+
+as_status launch_attend(as_ctx *ctx, AttendArgs a)
+{
+    const AttendPlan p = plan_of(ctx, a);
+    a.parts = p.parts;
+    a.sums = (float *)ctx->attend_parts.ptr;
+    a.stats = (float2 *)(a.sums + (size_t)a.tokens * a.heads * p.parts * a.dim);
+    for (int i = 0; i < p.count; ++i)
+        if (p.blocks[i] > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
+    for (int i = 0; i < p.count; ++i) {
+        const dim3 grid((unsigned)p.blocks[i], (unsigned)p.piece[i].parts);
+        if (a.dtype == AS_BF16) rows_of<uint16_t>(ctx, a, p.piece[i], grid);
+        else rows_of<float>(ctx, a, p.piece[i], grid);
+        AS_HIP_TRY(ctx, hipGetLastError());
+    }
+    if (a.parts > 1) {
+        const dim3 grid((unsigned)((a.tokens * a.heads + 3) / 4));
+        if (a.dtype == AS_BF16) hipLaunchKernelGGL(attend_join_kernel<uint16_t>, grid, dim3(256), 0, ctx->stream, a);
+        else hipLaunchKernelGGL(attend_join_kernel<float>, grid, dim3(256), 0, ctx->stream, a);
+        AS_HIP_TRY(ctx, hipGetLastError());
+    }
+    return AS_OK;
+}
+
+// ---------------------------------------------------------------- new tokens
+
+// Keys and values of new tokens into their sequences' pages, 16 bytes a thread and step: a token's heads lie one behind the other in
+// the rows that a product leaves, and a page apart in the cache.  Token i of sequence s's n new ones goes to position
+// lens[s] - n + i; what is outside the table or names no page is left out.
+__global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t tokens_each,
+                                                        int32_t esz)
+{
+    const int32_t per_head = a.dim * esz / 16, pieces = 2 * a.kv_heads * per_head;
+    int64_t s = 0, from = 0, to = 0, first;
+    if (a.offsets) {
+        s = find_sequence(a, blockIdx.x, 1, tokens_each);
+        from = offset_at(a, s);
+        to = offset_at(a, s + 1);
+        first = from + ((int64_t)blockIdx.x - s - from / tokens_each) * tokens_each;
+        if (first < from || first >= to || (a.finished && a.finished[s])) return;
+    } else {
+        first = (int64_t)blockIdx.x * tokens_each;
+        to = a.tokens;
+    }
+    const int32_t here = (int32_t)(to - first < tokens_each ? to - first : tokens_each);
+    for (int32_t i = threadIdx.x; i < here * pieces; i += 256) {
+        const int32_t t = i / pieces, x = i - t * pieces;
+        const int64_t token = first + t, seq = a.offsets ? s : token;
+        if (!a.offsets && a.finished && a.finished[seq]) continue;
+        const int64_t pos = (int64_t)a.lens[seq] - (a.offsets ? to - token : 1);
+        if (pos < 0 || pos >= a.room) continue;
+        const int32_t page = a.table[seq * a.table_ld + (pos >> a.page_shift)];
+        if (page < 0 || page >= a.pages) continue;
+        const bool value = x >= pieces / 2;
+        const int32_t y = value ? x - pieces / 2 : x, head = y / per_head, at = (y - head * per_head) * 16;
+        const char *const source = (const char *)(value ? v : k) + token * (value ? ldv : ldk) * esz + (int64_t)y * 16;
+        char *const target = (char *)const_cast<void *>(value ? a.v : a.k) + (int64_t)page * a.page_bytes +
+                             (((int64_t)head << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * (int64_t)(a.dim * esz) + at;
+        const u32x4_any in = *reinterpret_cast<const u32x4_any *>(source);
+        *reinterpret_cast<u32x4 *>(target) = u32x4{in[0], in[1], in[2], in[3]};
+    }
+}
+
+as_status launch_cache_add(as_ctx *ctx, const AttendArgs &a, const void *k, int64_t ldk, const void *v, int64_t ldv)
+{
+    const int32_t esz = a.dtype == AS_BF16 ? 2 : 4, pieces = 2 * a.kv_heads * (a.dim * esz / 16);
+    int32_t each = 2048 / pieces;
+    each = each < 1 ? 1 : each > 64 ? 64 : each;
+    const int64_t blocks = a.offsets ? a.tokens / each + a.rows : (a.tokens + each - 1) / each;
+    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more tokens than one launch takes");
+    hipLaunchKernelGGL(cache_add_kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a, k, ldk, v, ldv, each, esz);
+    AS_HIP_TRY(ctx, hipGetLastError());
+    return AS_OK;
+}
+
+}  // namespace as

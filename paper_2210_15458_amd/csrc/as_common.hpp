@@ -59,6 +59,7 @@ struct as_ctx {
     // many rows where decodes of their size have few, and neither is to move the other's
     as::DeviceBuf encode_logits, encode_state;
     as::DeviceBuf linear_x;        // as_linear: the rows of x that have to be laid out
+    as::DeviceBuf attend_parts;    // attention: what the parts of a split come to, until they are joined
     as::Profile prof;
     int step_shape = 0;            // work-group shape of the sampling kernel (tuning knob, 0 = default)
     // choices of a kernel (tuning knobs, 0 = by the rules on sizes)
@@ -358,6 +359,46 @@ struct HistoryArgs {
     const int32_t *lens;         // or null
 };
 
+struct AttendArgs {
+    const void *k, *v;           // [pages, kv_heads, page, dim]
+    int64_t pages, page_bytes;   // (from page to page)
+    int32_t page_shift, kv_heads, dim;
+    as_dtype dtype;
+    const void *q;               // [tokens, heads, dim], rows ldq apart
+    int64_t ldq;
+    void *out;
+    int64_t ldo;
+    int32_t heads, group;        // group: of a key head
+    float scale;                 // times log2(e)
+    int32_t window, sinks;       // window <= 0: none
+    int64_t rows;                // sequences
+    const int32_t *table;        // [rows, table_ld] pages, or null: no tokens of the rows' own
+    int64_t table_ld;
+    const int32_t *lens;
+    int32_t room;                // tokens that the table has pages for
+    const int32_t *prompt_table; // [prompts, prompt_table_ld], or null
+    int64_t prompt_table_ld;
+    const int32_t *prompt_lens;
+    int32_t prompt_room, per;    // per: rows of a prompt
+    const uint8_t *finished;     // [rows] or null
+    int64_t tokens;              // queries
+    const int64_t *offsets;      // [rows + 1] whose they are, or null: one a row
+    float *sums;                 // [tokens, heads, parts, dim] where there are parts to join ...
+    float2 *stats;               // [tokens, heads, parts] ... and their largest scores and sums of weights
+    int32_t parts;
+};
+enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
+struct AttendPiece {             // one launch: which keys and queries
+    int mode;
+    int32_t tiles;               // of queries, of a row or prompt
+    int32_t part0, parts;        // the parts that it leaves
+    int32_t least;               // tiles of keys that a part takes at least
+};
+constexpr int32_t kAttendMostParts = 32;
+
+size_t attend_workspace(const as_ctx *ctx, const AttendArgs &a);
+as_status launch_attend(as_ctx *ctx, AttendArgs a);
+as_status launch_cache_add(as_ctx *ctx, const AttendArgs &a, const void *k, int64_t ldk, const void *v, int64_t ldv);
 as_status launch_shape(as_ctx *ctx, const as_shaping &s, const void *logits, int64_t rows, int64_t ld, void *out, int64_t ldo);
 as_status launch_history_set(as_ctx *ctx, const HistoryArgs &a);
 as_status launch_history_add(as_ctx *ctx, const HistoryArgs &a, const int32_t *tokens, const uint8_t *finished);
