@@ -136,6 +136,8 @@ const char *as_last_error(const as_ctx *ctx);
  *                       same, 5 = 128 x 128, 6 = 256 x 256, 7, 8, 9 = up to 16
  *                       rows, in 2, 4, 8 shares of the sum; fp32 layers: 1..5 =
  *                       16 x 16, 16 x 32, 32 x 64, 64 x 64, 128 x 128
+ *   AS_TUNE_ATTEND_SHAPE  as_attend (prompts that rows share) and as_attend_prompts: queries of
+ *                       a work-group: 1 = 16, 2 = 128 (bf16 caches)
  */
 typedef enum {
     AS_TUNE_STEP_SHAPE = 0,
@@ -144,7 +146,8 @@ typedef enum {
     AS_TUNE_GEMM_GM = 3,
     AS_TUNE_WORKSPACE_MIB = 4,
     AS_TUNE_KEPT_ROWS = 5,
-    AS_TUNE_LINEAR_SHAPE = 6
+    AS_TUNE_LINEAR_SHAPE = 6,
+    AS_TUNE_ATTEND_SHAPE = 7
 } as_tuning;
 as_status as_ctx_set_tuning(as_ctx *ctx, as_tuning knob, int32_t value);
 

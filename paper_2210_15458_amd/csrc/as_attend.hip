@@ -13,9 +13,17 @@ namespace as {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNone = -__builtin_inff();
+
+// Two weights as bf16.  (By the compiler, not the instruction by hand: what an exponential has just left may be read by other
+// instructions only after a pause that the compiler sees to.)
+__device__ __forceinline__ uint32_t weights2(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
 
 // ---------------------------------------------------------------- which queries, which keys
 
@@ -194,22 +202,23 @@ template <class T> __device__ __forceinline__ uint32_t numbers(uint32_t x)
 
 // What a wave left out of its product: the values that are no numbers in the tiles that not every query sees whole, to the sums of
 // those that do see them (0 * NaN is NaN, so the product cannot leave them out by their weight).
-template <class T, int QUERIES, int EVERY>
-__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Work &w, const Keys &keys, int32_t BN, int32_t from, int32_t at,
-                                                         float *sums, int32_t stride)
+template <class T, int QUERIES>
+__device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Work &w, const Keys &keys, int32_t BN, int32_t from, int32_t every, int32_t at,
+                                               float *sums, int32_t stride, int32_t d0, int32_t d1)
 {
-    for (int32_t t = keys.first + from; t < keys.last; t += EVERY) {
+    for (int32_t t = keys.first + from; t < keys.last; t += every) {
         const int32_t base = keys.base(t, BN);
         if (keys.whole(base, BN)) continue;
         for (int32_t x = base; x < base + BN && x < keys.hi; ++x) {
             if (!keys.seen_by_some(x)) continue;
             const T *const row = (const T *)token_at(a.v, a, w, x, sizeof(T));
-            for (int32_t d = lane_id(); d - lane_id() < a.dim; d += kWave) {
-                const float y = d < a.dim ? widen(row[d]) : 0.f;
+            for (int32_t first = d0; first < d1; first += kWave) {
+                const int32_t d = first + lane_id();
+                const float y = d < d1 ? widen(row[d]) : 0.f;
                 const bool is = (__builtin_bit_cast(uint32_t, y) & 0x7f800000u) == 0x7f800000u;
                 if (!__any(is)) continue;
                 for (int q = 0; q < QUERIES; ++q)
-                    if (keys.seen(x, __builtin_amdgcn_readlane(at, q)) && is) sums[q * stride + d] += y;
+                    if (keys.seen(x, __builtin_amdgcn_readlane(at, q)) && is) sums[q * stride + d - d0] += y;
             }
         }
     }
@@ -415,7 +424,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
             u32x4 pw;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                pw[i] = pack2_bf16(p[2 * i], p[2 * i + 1]);
+                pw[i] = weights2(p[2 * i], p[2 * i + 1]);
                 l += __builtin_bit_cast(float, (uint32_t)pw[i] << 16) + __builtin_bit_cast(float, (uint32_t)pw[i] & 0xffff0000u);
             }
 #pragma unroll
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
                 *reinterpret_cast<f32x4 *>(to + e) = x;
             }
         }
-    if (odd) add_odd_values<T, 16, 4>(a, w, keys, BN, wave, at, sums + wave * 16 * kStride, kStride);
+    if (odd) add_odd_values<T, 16>(a, w, keys, BN, wave, 4, at, sums + wave * 16 * kStride, kStride, 0, a.dim);
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * (DP / 8); i += 256) {
         const int r = i / (DP / 8), d = i % (DP / 8) * 8;
@@ -495,6 +504,284 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
             if (d == 0) a.stats[at_part] = float2{top, total};
             if (top != kNone) store8(a.sums + at_part * a.dim + d, y);
         }
+    }
+}
+
+// ---------------------------------------------------------------- 128 queries a block, keys through LDS
+
+// Where many queries share a key head (a prompt's rows, a prompt's own tokens) the matrix instructions bound it, and the rate
+// at which operands reach them: four waves of 32 queries each share tiles of 64 keys (32 of 256 dimensions), which go from memory to LDS
+// without registers, the next tile's while this one is worked on.  As above both products are transposed,
+// on v_mfma_f32_32x32x16_bf16: S^T = K Q^T leaves register v of lane l the score of token 8 (v / 4) + 4 (l / 32) + v % 4 of 32 for query
+// l % 32; so a lane's P^T for 16 tokens is its registers 8 i .. 8 i + 7 in pairs, and V^T is read from LDS transposed
+// (ds_read_b64_tr_b16: of 16 lanes that read 4 rows of 16 values, each gets one column) for the same tokens.
+// In LDS a row's 16-byte pieces are exchanged (by its number, piece c at c ^ f(row)), so that neither the rows that 16 lanes
+// read of K nor the four rows they read of V meet in a bank.
+// A query's reference m is raised only when a score passes it by 2^8: weights up to 256 are as good as weights up to 1.
+template <int DP> struct TileForm {
+    static constexpr int kKeys = DP == 256 ? 32 : 64, kPieces = DP / 8, kBytes = kKeys * DP * 2, kLoads = kBytes / 4096, kRowsEach = 64 / kPieces;
+    static constexpr int kQueries = 128, kStride = 68;
+    static constexpr int kLds = 4 * kBytes > kQueries * kStride * 4 ? 4 * kBytes : kQueries * kStride * 4;
+    static __device__ __forceinline__ int key_place(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
+    static __device__ __forceinline__ int value_place(int row) { return DP == 64 ? (row >> 1 & 1) << 2 : (row & 3) << 2; }
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void glb_void;
+
+template <int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a, AttendPiece piece)
+{
+    typedef TileForm<DP> F;
+    constexpr int BN = F::kKeys, kLoads = F::kLoads, kPieces = F::kPieces, kStride = F::kStride, kRow = DP * 2;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[F::kLds];
+    __shared__ int64_t rows_at[F::kQueries];
+    __shared__ int32_t ends[2][4], any_odd;
+    const int lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t bytes = a.dim * 2;
+    // the last queries of a prompt see most keys: they start first
+    const int64_t item = piece.mode == kAttendRagged ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    Work w;
+    if (!find_work(a, piece.mode, F::kQueries, piece.tiles, wave * 32 + mine, item, w)) return;
+    const int32_t at = w.valid ? w.at : -1;
+    int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = at;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t u = __shfl_xor(lo_at, d, kWave), v = __shfl_xor(hi_at, d, kWave);
+        lo_at = u < lo_at ? u : lo_at;
+        hi_at = v > hi_at ? v : hi_at;
+    }
+    if (lane < 32) rows_at[wave * 32 + mine] = w.valid ? w.token * a.heads + w.qhead : -1;
+    if (lane == 0) {
+        ends[0][wave] = lo_at;
+        ends[1][wave] = hi_at;
+    }
+    if (threadIdx.x == 0) any_odd = 0;
+    if (!FULL) {                                       // what lies past the rows' ends is never written to again
+        for (int i = threadIdx.x; i < 4 * F::kBytes / 16; i += 256) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    }
+    const int32_t wave_lo = __builtin_amdgcn_readfirstlane(lo_at), wave_hi = __builtin_amdgcn_readfirstlane(hi_at);
+    // the queries (zeros where there is none and past the row's end)
+    u32x4 q[DP / 16];
+    {
+        const char *const from = (const char *)a.q + (w.token * a.ldq + (int64_t)w.qhead * a.dim) * 2;
+        const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const int32_t o = (i * 2 + half) * 16;
+            q[i] = u32x4{0, 0, 0, 0};
+            if (w.valid && a.scale != 0.f && (FULL || o < bytes)) q[i] = *reinterpret_cast<const u32x4_any *>(from + o);
+            q[i] ^= sign;
+        }
+    }
+    const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
+    __syncthreads();
+    int32_t lo = ends[0][0], hi = ends[1][0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        lo = ends[0][i] < lo ? ends[0][i] : lo;
+        hi = ends[1][i] > hi ? ends[1][i] : hi;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    if (lo > hi) lo = hi;
+    const Keys keys = keys_of(a, w, lo, hi, BN, blockIdx.y, piece.parts, piece.least);
+
+    // what a lane fetches: of each of its wave's kLoads KiB of a tile 16 bytes, which land in its place
+    const int row0 = wave * F::kRowsEach + lane / kPieces;            // (load i: 4 i kRowsEach further on)
+    auto piece_of = [&](int place) __attribute__((always_inline)) { return ((lane % kPieces) ^ place) * 16; };
+    int32_t page[kLoads];                              // of the tile to be fetched next
+    auto find_pages = [&](int32_t t) __attribute__((always_inline)) {
+        if (t >= keys.last) return;
+        const int32_t base = keys.base(t, BN);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if constexpr (BYPAGE) {
+                const int32_t first = base + (4 * i + wave) * F::kRowsEach, there = first < keys.n ? first : base;
+                page[i] = scalar_load(w.table + (there >> a.page_shift));
+            } else {
+                const int32_t x = base + row0 + 4 * i * F::kRowsEach;
+                page[i] = w.table[(x < keys.n ? x : keys.n - 1) >> a.page_shift];
+            }
+            page[i] = page[i] < 0 ? 0 : page[i] < a.pages ? page[i] : (int32_t)a.pages - 1;
+        }
+    };
+    auto fetch = [&](int32_t t, int buffer) __attribute__((always_inline)) {
+        const int32_t base = keys.base(t, BN), mask = (1 << a.page_shift) - 1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int64_t off;
+            if constexpr (BYPAGE) {
+                const int32_t first = base + (4 * i + wave) * F::kRowsEach, there = first < keys.n ? first : base;
+                off = (int64_t)page[i] * a.page_bytes + (((int64_t)w.head << a.page_shift) + (there & mask)) * (int64_t)bytes;
+            } else {
+                const int32_t x = base + row0 + 4 * i * F::kRowsEach, there = x < keys.n ? x : keys.n - 1;
+                off = (int64_t)page[i] * a.page_bytes + (((int64_t)w.head << a.page_shift) + (there & mask)) * (int64_t)bytes;
+            }
+            const int row = row0 + 4 * i * F::kRowsEach;
+            const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
+            const int32_t ko = piece_of(F::key_place(row)), vo = piece_of(F::value_place(row));
+            unsigned char *const to = smem + buffer * F::kBytes + (4 * i + wave) * 1024;
+            if (FULL || ko < bytes)
+                __builtin_amdgcn_global_load_lds((glb_void *)((const char *)a.k + off + (in_rows + ko)), (lds_void *)to, 16, 0, 0);
+            if (FULL || vo < bytes)
+                __builtin_amdgcn_global_load_lds((glb_void *)((const char *)a.v + off + (in_rows + vo)), (lds_void *)(to + 2 * F::kBytes), 16, 0, 0);
+        }
+    };
+
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    float m = kNone, l = 0.f;
+    if (keys.first < keys.last) {
+        find_pages(keys.first);
+        fetch(keys.first, 0);
+        find_pages(keys.first + 1);
+    }
+#pragma unroll 1
+    for (int32_t t = keys.first; t < keys.last; ++t) {
+        const int buffer = (t - keys.first) & 1;
+        const int32_t base = keys.base(t, BN);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if (t + 1 < keys.last) {
+            fetch(t + 1, buffer ^ 1);
+            find_pages(t + 2);
+        }
+        unsigned char *const ks = smem + buffer * F::kBytes, *const vs = ks + 2 * F::kBytes;
+        if (!keys.whole(base, BN)) {
+            // what no query sees may be anything, and 0 * NaN is NaN; what is no number and seen by some alone is added at the end
+            for (int i = threadIdx.x; i < BN * kPieces; i += 256) {
+                u32x4 *const p = reinterpret_cast<u32x4 *>(vs) + i;
+                if (!keys.seen_by_some(base + i / kPieces)) *p = u32x4{0, 0, 0, 0};
+                else if (lo != hi) {
+                    u32x4 x = *p;
+                    uint32_t largest = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) largest = larger_magnitude<uint16_t>(largest, x[e]);
+                    if (no_number<uint16_t>(largest)) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = numbers<uint16_t>(x[e]);
+                        *p = x;
+                        any_odd = 1;
+                    }
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+        }
+        if (base > wave_hi) continue;                  // (the last tiles of a prompt's diagonal, for its first queries; no queries)
+
+        // scores
+        f32x16 s[BN / 32];
+        const unsigned char *const krow = ks + mine * kRow;
+        const int kx = (half ^ F::key_place(mine)) * 16;
+#pragma unroll
+        for (int b = 0; b < BN / 32; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(krow + b * 32 * kRow + ((i * 32) ^ kx));
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q[i]), s[b], 0, 0, 0);
+            }
+        }
+        if (!(base + BN <= keys.n && base + BN - 1 <= wave_lo && (a.window <= 0 || base > wave_hi - a.window || base + BN <= keys.sinks))) {
+#pragma unroll
+            for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[b][r] = keys.seen(base + b * 32 + 8 * (r >> 2) + 4 * half + (r & 3), at) ? s[b][r] : kNone;
+        }
+        float top = kNone;
+#pragma unroll
+        for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        top = top == kNone ? kNone : top * scale;
+        if (__any(top > m + 8.f)) {
+            const float now = fmaxf(top, m);
+            const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) o[i] *= by;
+        }
+        const float ref = m == kNone ? 0.f : m;
+        // weights, rounded to bf16 for the second product; l adds up the rounded ones, so that they come to 1 all the same
+#pragma unroll
+        for (int i = 0; i < BN / 16; ++i) {
+            u32x4 pw;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = s[i >> 1][(i & 1) * 8 + 2 * e], y = s[i >> 1][(i & 1) * 8 + 2 * e + 1];
+                pw[e] = weights2(__builtin_amdgcn_exp2f(fmaf(x, scale, -ref)), __builtin_amdgcn_exp2f(fmaf(y, scale, -ref)));
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)pw[e]), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+            }
+            const int vrow = 4 * half + (lane & 15) / 4;
+            const unsigned char *const from = vs + vrow * kRow + (lane & 1) * 8;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                const int c = (d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ F::value_place(vrow);
+                const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(from + i * 16 * kRow + c * 16));
+                const bf16x4 v1 =
+                    __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(from + (i * 16 + 8) * kRow + c * 16));
+                const bf16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pw), o[d], 0, 0, 0);
+            }
+        }
+    }
+
+    // sums to memory, 64 dimensions of a wave's queries at a time through its part of LDS
+    l += __shfl_xor(l, 32, kWave);
+    if (l != l && m == kNone) m = 0.f;
+    __syncthreads();
+    const bool odd = any_odd != 0;
+    float *const sums = reinterpret_cast<float *>(smem) + wave * 32 * kStride;
+    const float by = a.parts > 1 ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) {
+        if (c * 64 >= a.dim) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                f32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = o[c * 2 + i][r + e] * by;
+                *reinterpret_cast<f32x4 *>(sums + mine * kStride + i * 32 + 2 * r + 4 * half) = x;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        if (odd) add_odd_values<uint16_t, 32>(a, w, keys, BN, 0, 1, at, sums, kStride, c * 64, c * 64 + 64 < a.dim ? c * 64 + 64 : a.dim);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + lane / 8, d = c * 64 + lane % 8 * 8;
+            const int64_t row = rows_at[wave * 32 + r];
+            const float ml = __shfl(m, r, kWave), ll = __shfl(l, r, kWave);
+            if (row < 0 || d >= a.dim) continue;
+            float y[8];
+            const float *const from = sums + r * kStride + lane % 8 * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = from[e];
+            if (a.parts == 1) {
+                const int64_t token = row / a.heads;
+                store8((uint16_t *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
+            } else {
+                const int64_t at_part = row * a.parts + piece.part0 + blockIdx.y;
+                if (d == 0) a.stats[at_part] = float2{ml, ll};
+                if (ml != kNone) store8(a.sums + at_part * a.dim + d, y);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -548,6 +835,19 @@ static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3
     else if (a.dim != DP) hipLaunchKernelGGL((attend_rows_kernel<T, DP, false, true>), grid, dim3(256), 0, ctx->stream, a, p);
     else hipLaunchKernelGGL((attend_rows_kernel<T, DP, true, true>), grid, dim3(256), 0, ctx->stream, a, p);
 }
+template <int DP>
+static void tiles_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+{
+    if (a.page_shift < 4) hipLaunchKernelGGL((attend_tiles_kernel<DP, false, false>), grid, dim3(256), 0, ctx->stream, a, p);
+    else if (a.dim != DP) hipLaunchKernelGGL((attend_tiles_kernel<DP, false, true>), grid, dim3(256), 0, ctx->stream, a, p);
+    else hipLaunchKernelGGL((attend_tiles_kernel<DP, true, true>), grid, dim3(256), 0, ctx->stream, a, p);
+}
+static void tiles_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+{
+    if (a.dim <= 64) tiles_of<64>(ctx, a, p, grid);
+    else if (a.dim <= 128) tiles_of<128>(ctx, a, p, grid);
+    else tiles_of<256>(ctx, a, p, grid);
+}
 template <class T>
 static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
 {
@@ -575,25 +875,32 @@ static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room)
 static AttendPlan plan_of(const as_ctx *ctx, const AttendArgs &a)
 {
     AttendPlan p;
-    auto add = [&](int mode, int64_t blocks, int32_t tiles, int64_t room) {
+    auto add = [&](int mode, int queries, int64_t blocks, int32_t tiles, int64_t room) {
         AttendPiece &x = p.piece[p.count];
         x.mode = mode;
+        x.queries = queries;
         x.tiles = tiles;
-        x.least = 8;
+        x.least = queries == 16 ? 8 : 4;
         x.part0 = p.parts;
         x.parts = parts_for(ctx, blocks, room);
         p.parts += x.parts;
         p.blocks[p.count++] = blocks;
     };
-    if (a.offsets) add(kAttendRagged, (a.tokens * a.group / 16 + a.rows) * a.kv_heads, 1, a.room);
-    else {
+    // many queries that share a key head: by tiles of 128
+    const bool bf16 = a.dtype == AS_BF16;
+    if (a.offsets) {
+        const int queries = bf16 && ctx->attend_shape != 1 && (ctx->attend_shape == 2 || a.tokens * a.group >= 32 * a.rows) ? 128 : 16;
+        add(kAttendRagged, queries, (a.tokens * a.group / queries + a.rows) * a.kv_heads, 1, a.room);
+    } else {
         if (a.prompt_table) {
-            const int32_t tiles = (int32_t)((a.per * (int64_t)a.group + 15) / 16);
-            add(kAttendShared, (a.rows + a.per - 1) / a.per * a.kv_heads * tiles, tiles, a.prompt_room);
+            const int64_t all = a.per * (int64_t)a.group;
+            const int queries = bf16 && ctx->attend_shape != 1 && (ctx->attend_shape == 2 || all >= 32) ? 128 : 16;
+            const int32_t tiles = (int32_t)((all + queries - 1) / queries);
+            add(kAttendShared, queries, (a.rows + a.per - 1) / a.per * a.kv_heads * tiles, tiles, a.prompt_room);
         }
         if (a.table) {
             const int32_t tiles = (a.group + 15) / 16;
-            add(kAttendOwn, a.rows * a.kv_heads * tiles, tiles, a.room);
+            add(kAttendOwn, 16, a.rows * a.kv_heads * tiles, tiles, a.room);
         }
     }
     return p;
@@ -615,7 +922,8 @@ as_status launch_attend(as_ctx *ctx, AttendArgs a)
         if (p.blocks[i] > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
     for (int i = 0; i < p.count; ++i) {
         const dim3 grid((unsigned)p.blocks[i], (unsigned)p.piece[i].parts);
-        if (a.dtype == AS_BF16) rows_of<uint16_t>(ctx, a, p.piece[i], grid);
+        if (p.piece[i].queries == 128) tiles_of(ctx, a, p.piece[i], grid);
+        else if (a.dtype == AS_BF16) rows_of<uint16_t>(ctx, a, p.piece[i], grid);
         else rows_of<float>(ctx, a, p.piece[i], grid);
         AS_HIP_TRY(ctx, hipGetLastError());
     }

@@ -70,6 +70,7 @@ struct as_ctx {
                                    // 4 = no table of all, 5 = one of the tokens that come
     int workspace_mib = 0;         // largest buffer of the workspace, in MiB (tuning knob: 0 = as large as the device gives)
     int linear_shape = 0;          // as_linear: the tile of a block (tuning knob, 0 = by the rule on sizes)
+    int attend_shape = 0;          // attention: 1 = 16 queries a block, 2 = 128 wherever there may be more than 16 (bf16; tuning knob, 0 = by the rule)
     int num_cus = 0;               // compute units of the device (the persistent logits kernel runs one block on each)
     std::string err;
 };
@@ -389,7 +390,7 @@ struct AttendArgs {
 };
 enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
 struct AttendPiece {             // one launch: which keys and queries
-    int mode;
+    int mode, queries;           // queries: of a block
     int32_t tiles;               // of queries, of a row or prompt
     int32_t part0, parts;        // the parts that it leaves
     int32_t least;               // tiles of keys that a part takes at least

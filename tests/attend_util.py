@@ -14,7 +14,8 @@ class Batch:
 
     def __init__(self, own, dim, kv_heads, page, dtype, prompts=None, per=1, seed=0, spare=2, room=None, value=1.0):
         self.g = torch.Generator(device="cuda").manual_seed(seed)
-        self.dim, self.kv_heads, self.page, self.dtype, self.per = dim, kv_heads, page, DTYPES[dtype], per
+        self.dim, self.kv_heads, self.page, self.dtype, self.per = dim, kv_heads, page, DTYPES[dtype.split()[0]], per
+        self.shape = {"16": 1, "128": 2}.get(dtype.split()[-1], 0)
         self.own, self.prompts = list(own), prompts
         both = self.own + (prompts or [])
         need = [-(-n // page) for n in both]

@@ -8,6 +8,8 @@ from paper_2210_15458_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
+FORMS = ["bf16", "bf16 16", "bf16 128", "f32"]     # (the last number: queries of a work-group, whatever the rule would have)
+
 
 def run(batch, heads, window=0, sinks=0, scale=None, finished=None, pad=0, ctx=None, seed=5, gain=1.5, q=None):
     rows, dim = len(batch.own), batch.dim
@@ -17,6 +19,8 @@ def run(batch, heads, window=0, sinks=0, scale=None, finished=None, pad=0, ctx=N
         q = wide[:, pad // 2:pad // 2 + heads * dim]
     out = torch.full((rows, heads * dim + pad), 7.0, dtype=batch.dtype, device="cuda")
     ctx = ctx or B.Ctx(max(rows, 1), 100, torch.float32)
+    if batch.shape:
+        ctx.set_tuning("attend_shape", batch.shape)
     seqs = B.Sequences(rows, batch.table, batch.lens, batch.prompt_table, batch.prompt_lens, batch.per, finished)
     B.as_attend(ctx, B.Cache(batch.k, batch.v), seqs, q, out[:, pad // 2:pad // 2 + heads * dim], scale=scale, window=window, sinks=sinks)
     torch.cuda.synchronize()
@@ -25,7 +29,7 @@ def run(batch, heads, window=0, sinks=0, scale=None, finished=None, pad=0, ctx=N
     return q, out[:, pad // 2:pad // 2 + heads * dim]
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,kv_heads,group,page", [(64, 2, 4, 16), (128, 1, 1, 16), (128, 3, 8, 64), (256, 2, 2, 16), (8, 1, 3, 4), (72, 2, 5, 1),
                                                      (136, 1, 16, 8), (96, 2, 17, 32), (128, 1, 33, 2), (200, 1, 4, 128), (64, 5, 1, 1024)])
 def test_lengths(dtype, dim, kv_heads, group, page):
@@ -35,7 +39,7 @@ def test_lengths(dtype, dim, kv_heads, group, page):
     print("worst", check(out, q, b))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,group,page,window,sinks", [(64, 2, 16, 1, 0), (128, 4, 16, 5, 1), (128, 1, 4, 32, 0), (72, 3, 16, 33, 40), (64, 8, 32, 100, 7),
                                                          (256, 2, 64, 64, 64), (128, 4, 16, 1000, 3), (64, 1, 16, 2147483647, 2147483647)])
 def test_windows_and_first_tokens(dtype, dim, group, page, window, sinks):
@@ -50,7 +54,7 @@ def test_windows_and_first_tokens(dtype, dim, group, page, window, sinks):
     print("worst", check(out, q, b, window=window, sinks=sinks))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,kv_heads,group,page,per", [(64, 2, 4, 16, 4), (128, 1, 1, 16, 33), (72, 2, 3, 8, 5), (128, 2, 8, 64, 16), (256, 1, 2, 16, 70)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3), (7, 200)])
 def test_prompts_shared_by_rows(dtype, dim, kv_heads, group, page, per, window, sinks):
@@ -63,7 +67,7 @@ def test_prompts_shared_by_rows(dtype, dim, kv_heads, group, page, per, window, 
     print("worst", check(out, q, b, window=window, sinks=sinks, rows=rows))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 def test_prompts_alone_and_split(dtype):
     """No tokens of the rows' own; one row over a long prompt, whose keys are split and joined."""
     b = Batch([0, 0], 128, 2, 16, dtype, prompts=[5000], per=2, seed=3)
@@ -72,7 +76,7 @@ def test_prompts_alone_and_split(dtype):
     print("worst", check(out, q, b))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 0), (1500, 2000), (20000, 5)])
 def test_long_split(dtype, window, sinks):
     b = Batch([9000, 1, 4097, 0, 12345], 64, 1, 16, dtype, seed=9, room=2000)
@@ -80,7 +84,7 @@ def test_long_split(dtype, window, sinks):
     print("worst", check(out, q, b, window=window, sinks=sinks))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("prompts", [None, [100, 20]])
 def test_finished_rows_are_left_as_they_were(dtype, prompts):
     own = [40, 3, 0, 700, 64, 9]
@@ -91,7 +95,7 @@ def test_finished_rows_are_left_as_they_were(dtype, prompts):
     check(out, q, b, rows=[0, 2, 3])
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("per", [3, 40])
 def test_no_numbers_reach_those_that_see_them_only(dtype, per):
     """A value of the prompt that is infinite or NaN, in the window of some rows and not of others; a NaN in one row's query."""
@@ -137,7 +141,7 @@ def test_no_numbers_reach_those_that_see_them_only(dtype, per):
 
 def test_steep_and_flat_scores():
     """Scores far beyond what an exponential without a maximum taken off could hold, and all alike."""
-    for dtype in ("bf16", "f32"):
+    for dtype in FORMS:
         b = Batch([200, 77], 64, 1, 16, dtype, seed=4)
         q, out = run(b, 2, gain=60.0, scale=1.0)
         check(out, q, b, scale=1.0)

@@ -8,6 +8,8 @@ from paper_2210_15458_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
+FORMS = ["bf16", "bf16 16", "bf16 128", "f32"]     # (the last number: queries of a work-group, whatever the rule would have)
+
 
 def run(batch, new, heads, window=0, sinks=0, finished=None, pad=0, before=0, behind=3, seed=5, q=None, ctx=None, scale=None):
     """new: queries of each row; before, behind: rows of q and out that are nobody's."""
@@ -20,6 +22,8 @@ def run(batch, new, heads, window=0, sinks=0, finished=None, pad=0, before=0, be
         offsets.append(offsets[-1] + x)
     out = torch.full((n, heads * dim + pad), 7.0, dtype=batch.dtype, device="cuda")
     ctx = ctx or B.Ctx(max(n, len(new)), 100, torch.float32)
+    if batch.shape:
+        ctx.set_tuning("attend_shape", batch.shape)
     seqs = B.Sequences(len(new), batch.table, batch.lens, finished=finished)
     B.as_attend_prompts(ctx, B.Cache(batch.k, batch.v), seqs, q, torch.tensor(offsets, device="cuda"), out[:, pad // 2:pad // 2 + heads * dim],
                         window=window, sinks=sinks, scale=scale)
@@ -30,7 +34,7 @@ def run(batch, new, heads, window=0, sinks=0, finished=None, pad=0, before=0, be
     return q, out[:, pad // 2:pad // 2 + heads * dim], offsets
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,kv_heads,group,page", [(64, 2, 4, 16), (128, 1, 1, 16), (128, 2, 8, 64), (256, 1, 2, 16), (8, 1, 3, 4), (72, 2, 5, 1),
                                                      (136, 1, 16, 8), (96, 1, 17, 32), (200, 1, 4, 128), (64, 3, 1, 1024)])
 def test_chunks(dtype, dim, kv_heads, group, page):
@@ -41,7 +45,7 @@ def test_chunks(dtype, dim, kv_heads, group, page):
     print("worst", check(out, q, b, offsets=offsets))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,group,page,window,sinks", [(64, 2, 16, 1, 0), (128, 4, 16, 5, 1), (128, 1, 4, 32, 0), (72, 3, 16, 33, 40), (64, 8, 32, 100, 7),
                                                          (256, 2, 64, 64, 64), (128, 4, 16, 1000, 3), (128, 2, 16, 129, 100)])
 def test_windows_and_first_tokens(dtype, dim, group, page, window, sinks):
@@ -56,7 +60,7 @@ def test_windows_and_first_tokens(dtype, dim, group, page, window, sinks):
     print("worst", check(out, q, b, window=window, sinks=sinks, offsets=offsets))
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("had,new", [(0, 700), (6000, 5), (3000, 400)])
 def test_long(dtype, had, new):
     b = Batch([had + new, 3], 128, 2, 16, dtype, seed=had, room=700)
@@ -79,7 +83,7 @@ class Shorter:
         return [x[:, :self.n] for x in self.batch.tokens(r)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 def test_no_numbers_of_later_tokens_stay_there(dtype):
     """A token whose value is infinite or NaN: queries before it do not see it, those behind it do until a window leaves it."""
     for window, sinks in ((0, 0), (20, 0), (20, 3)):
@@ -115,7 +119,7 @@ def test_no_numbers_of_later_tokens_stay_there(dtype):
         check(out2, q2, b, window=window, sinks=sinks, offsets=offsets)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", FORMS)
 def test_a_query_that_is_no_number_stays_alone(dtype):
     b = Batch([100], 128, 1, 16, dtype, seed=12)
     q, out, offsets = run(b, [100], 2)
