@@ -241,21 +241,28 @@ template <int DP> struct AttendForm<float, DP> {
     static constexpr int kSub = 1, kKey = DP / 16, kVBytes = 16, kChunks = DP / 64, kEach = 4;
 };
 
+template <class T, int DP> struct RowsShared {
+    static constexpr int kStride = DP + 4;
+    __attribute__((aligned(16))) float sums[4 * 16 * kStride];
+    float2 stats[4][16];
+    int64_t rows_at[16];                               // token * heads + head of each query, -1: none
+};
+
 template <class T, int DP, bool FULL, bool BYPAGE>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPiece piece)
+__device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPiece &piece, int64_t item, int32_t part, RowsShared<T, DP> &shared)
 {
     typedef AttendForm<T, DP> F;
     constexpr int kSub = F::kSub, kKey = F::kKey, kVBytes = F::kVBytes, kChunks = F::kChunks, kEach = F::kEach, BN = 16 * kSub;
     constexpr int kStride = DP + 4, kWords = kVBytes / 4;
     constexpr bool kBf16 = sizeof(T) == 2;
-    __shared__ __attribute__((aligned(16))) float sums[4 * 16 * kStride];
-    __shared__ float2 stats[4][16];
-    __shared__ int64_t rows_at[16];                    // token * heads + head of each query, -1: none
+    float *const sums = shared.sums;
+    float2(*const stats)[16] = shared.stats;
+    int64_t *const rows_at = shared.rows_at;
     const int lane = threadIdx.x & 63, quarter = lane >> 4, mine = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * (int32_t)sizeof(T);
     Work w;
-    if (!find_work(a, piece.mode, 16, piece.tiles, mine, blockIdx.x, w)) return;
+    if (!find_work(a, piece.mode, 16, piece.tiles, mine, item, w)) return;
     int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = w.valid ? w.at : -1;
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
@@ -266,7 +273,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
     lo_at = __builtin_amdgcn_readfirstlane(lo_at);
     hi_at = __builtin_amdgcn_readfirstlane(hi_at);
     if (lo_at > hi_at) lo_at = hi_at;                  // (no query)
-    const Keys keys = keys_of(a, w, lo_at, hi_at, BN, blockIdx.y, piece.parts, piece.least);
+    const Keys keys = keys_of(a, w, lo_at, hi_at, BN, part, piece.parts, piece.least);
     const int32_t at = w.valid ? w.at : -1;
 
     // the queries, zeros where there is none and past the row's end
@@ -500,7 +507,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
             const int64_t token = row / a.heads;
             store8((T *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
         } else {
-            const int64_t at_part = row * a.parts + piece.part0 + blockIdx.y;
+            const int64_t at_part = row * a.parts + piece.part0 + part;
             if (d == 0) a.stats[at_part] = float2{top, total};
             if (top != kNone) store8(a.sums + at_part * a.dim + d, y);
         }
@@ -531,19 +538,24 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void glb_void;
 
+template <int DP> struct TilesShared {
+    __attribute__((aligned(1024))) unsigned char smem[TileForm<DP>::kLds];
+    int64_t rows_at[TileForm<DP>::kQueries];
+    int32_t ends[2][4], any_odd;
+};
+
 template <int DP, bool FULL, bool BYPAGE>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a, AttendPiece piece)
+__device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPiece &piece, int64_t item, int32_t part, TilesShared<DP> &shared)
 {
     typedef TileForm<DP> F;
     constexpr int BN = F::kKeys, kLoads = F::kLoads, kPieces = F::kPieces, kStride = F::kStride, kRow = DP * 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[F::kLds];
-    __shared__ int64_t rows_at[F::kQueries];
-    __shared__ int32_t ends[2][4], any_odd;
+    unsigned char *const smem = shared.smem;
+    int64_t *const rows_at = shared.rows_at;
+    int32_t(*const ends)[4] = shared.ends;
+    int32_t &any_odd = shared.any_odd;
     const int lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * 2;
-    // the last queries of a prompt see most keys: they start first
-    const int64_t item = piece.mode == kAttendRagged ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     Work w;
     if (!find_work(a, piece.mode, F::kQueries, piece.tiles, wave * 32 + mine, item, w)) return;
     const int32_t at = w.valid ? w.at : -1;
@@ -588,7 +600,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(At
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
     if (lo > hi) lo = hi;
-    const Keys keys = keys_of(a, w, lo, hi, BN, blockIdx.y, piece.parts, piece.least);
+    const Keys keys = keys_of(a, w, lo, hi, BN, part, piece.parts, piece.least);
 
     // what a lane fetches: of each of its wave's kLoads KiB of a tile 16 bytes, which land in its place
     const int row0 = wave * F::kRowsEach + lane / kPieces;            // (load i: 4 i kRowsEach further on)
@@ -776,12 +788,90 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(At
                 const int64_t token = row / a.heads;
                 store8((uint16_t *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
             } else {
-                const int64_t at_part = row * a.parts + piece.part0 + blockIdx.y;
+                const int64_t at_part = row * a.parts + piece.part0 + part;
                 if (d == 0) a.stats[at_part] = float2{ml, ll};
                 if (ml != kNone) store8(a.sums + at_part * a.dim + d, y);
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---------------------------------------------------------------- launches of both
+
+// Which work is block b's: of a piece's items, of which `tiles` after each other read the same keys, those of a group go to one
+// XCD (blocks go round the eight), whose L2 then has the keys; of ragged queries the last first, which see most keys.
+__device__ __forceinline__ void item_of(const AttendPiece &p, int64_t b, int64_t *item, int32_t *part)
+{
+    const int64_t groups = p.blocks / p.tiles * p.parts, whole = groups & ~(int64_t)7;
+    if (p.mode == kAttendRagged) {
+        *part = (int32_t)(b / p.blocks);
+        *item = p.blocks - 1 - (b - *part * p.blocks);
+        return;
+    }
+    int64_t group;
+    int32_t tile;
+    if (b < whole * p.tiles) {
+        const int64_t j = b >> 3;
+        tile = (int32_t)(j % p.tiles);
+        group = j / p.tiles * 8 + (b & 7);
+    } else {
+        tile = (int32_t)(b % p.tiles);
+        group = b / p.tiles;
+    }
+    *part = (int32_t)(group / (p.blocks / p.tiles));
+    *item = (group - *part * (p.blocks / p.tiles)) * p.tiles + tile;
+}
+
+// With two pieces (what rows share, and their own) every `every`-th block is one of the first, as long as there are any.
+__device__ __forceinline__ bool first_piece(const AttendPieces &p, int64_t *b)
+{
+    if (p.count < 2) return true;
+    const int64_t all = p.piece[0].blocks * p.piece[0].parts, turn = *b / p.every;
+    if (turn < all && *b == turn * p.every) {
+        *b = turn;
+        return true;
+    }
+    *b -= turn < all ? turn + 1 : all;
+    return false;
+}
+
+template <class T, int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPieces p)
+{
+    __shared__ RowsShared<T, DP> shared;
+    int64_t b = blockIdx.x, item;
+    int32_t part;
+    const AttendPiece &piece = first_piece(p, &b) ? p.piece[0] : p.piece[1];
+    item_of(piece, b, &item, &part);
+    attend_rows<T, DP, FULL, BYPAGE>(a, piece, item, part, shared);
+}
+
+template <int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a, AttendPieces p)
+{
+    __shared__ TilesShared<DP> shared;
+    int64_t item;
+    int32_t part;
+    item_of(p.piece[0], blockIdx.x, &item, &part);
+    attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared);
+}
+
+template <int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_both_kernel(AttendArgs a, AttendPieces p)
+{
+    __shared__ union Shared {
+        TilesShared<DP> tiles;
+        RowsShared<uint16_t, DP> rows;
+    } shared;
+    int64_t b = blockIdx.x, item;
+    int32_t part;
+    if (first_piece(p, &b)) {
+        item_of(p.piece[0], b, &item, &part);
+        attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared.tiles);
+    } else {
+        item_of(p.piece[1], b, &item, &part);
+        attend_rows<uint16_t, DP, FULL, BYPAGE>(a, p.piece[1], item, part, shared.rows);
     }
 }
 
@@ -828,63 +918,59 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     }
 }
 
+template <class T, int DP, bool FULL, bool BYPAGE>
+static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (p.piece[0].queries == 128 && p.count == 2) {
+            hipLaunchKernelGGL((attend_both_kernel<DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
+            return;
+        }
+        if (p.piece[0].queries == 128) {
+            hipLaunchKernelGGL((attend_tiles_kernel<DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((attend_rows_kernel<T, DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
+}
 template <class T, int DP>
-static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
 {
-    if (a.page_shift < 4) hipLaunchKernelGGL((attend_rows_kernel<T, DP, false, false>), grid, dim3(256), 0, ctx->stream, a, p);
-    else if (a.dim != DP) hipLaunchKernelGGL((attend_rows_kernel<T, DP, false, true>), grid, dim3(256), 0, ctx->stream, a, p);
-    else hipLaunchKernelGGL((attend_rows_kernel<T, DP, true, true>), grid, dim3(256), 0, ctx->stream, a, p);
-}
-template <int DP>
-static void tiles_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
-{
-    if (a.page_shift < 4) hipLaunchKernelGGL((attend_tiles_kernel<DP, false, false>), grid, dim3(256), 0, ctx->stream, a, p);
-    else if (a.dim != DP) hipLaunchKernelGGL((attend_tiles_kernel<DP, false, true>), grid, dim3(256), 0, ctx->stream, a, p);
-    else hipLaunchKernelGGL((attend_tiles_kernel<DP, true, true>), grid, dim3(256), 0, ctx->stream, a, p);
-}
-static void tiles_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
-{
-    if (a.dim <= 64) tiles_of<64>(ctx, a, p, grid);
-    else if (a.dim <= 128) tiles_of<128>(ctx, a, p, grid);
-    else tiles_of<256>(ctx, a, p, grid);
+    if (a.page_shift < 4) launch_pieces<T, DP, false, false>(ctx, a, p, grid);
+    else if (a.dim != DP) launch_pieces<T, DP, false, true>(ctx, a, p, grid);
+    else launch_pieces<T, DP, true, true>(ctx, a, p, grid);
 }
 template <class T>
-static void rows_of(as_ctx *ctx, const AttendArgs &a, const AttendPiece &p, dim3 grid)
+static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
 {
-    if (a.dim <= 64) rows_of<T, 64>(ctx, a, p, grid);
-    else if (a.dim <= 128) rows_of<T, 128>(ctx, a, p, grid);
-    else rows_of<T, 256>(ctx, a, p, grid);
+    if (a.dim <= 64) launch_pieces<T, 64>(ctx, a, p, grid);
+    else if (a.dim <= 128) launch_pieces<T, 128>(ctx, a, p, grid);
+    else launch_pieces<T, 256>(ctx, a, p, grid);
 }
 
-// What a call comes to: the launches, and the parts that each leaves.
-struct AttendPlan {
-    AttendPiece piece[2];
-    int64_t blocks[2];
-    int count = 0;
-    int32_t parts = 0;
-};
-
-static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room)
+// Parts that the keys of each query are split into: two blocks a compute unit, if each still has so many keys.
+static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room, int64_t least)
 {
     int64_t n = (2 * (int64_t)ctx->num_cus + blocks - 1) / blocks;
-    const int64_t most = (room + 255) / 256;
+    const int64_t most = (room + least - 1) / least;
     n = n < most ? n : most;
     return (int32_t)(n < 1 ? 1 : n > kAttendMostParts ? kAttendMostParts : n);
 }
 
-static AttendPlan plan_of(const as_ctx *ctx, const AttendArgs &a)
+static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *parts)
 {
-    AttendPlan p;
-    auto add = [&](int mode, int queries, int64_t blocks, int32_t tiles, int64_t room) {
-        AttendPiece &x = p.piece[p.count];
+    AttendPieces p{};
+    *parts = 0;
+    auto add = [&](int mode, int queries, int64_t groups, int32_t tiles, int64_t room) {
+        AttendPiece &x = p.piece[p.count++];
         x.mode = mode;
         x.queries = queries;
         x.tiles = tiles;
         x.least = queries == 16 ? 8 : 4;
-        x.part0 = p.parts;
-        x.parts = parts_for(ctx, blocks, room);
-        p.parts += x.parts;
-        p.blocks[p.count++] = blocks;
+        x.part0 = *parts;
+        x.blocks = groups * tiles;
+        x.parts = parts_for(ctx, x.blocks, room, queries == 16 ? 256 : 512);
+        *parts += x.parts;
     };
     // many queries that share a key head: by tiles of 128
     const bool bf16 = a.dtype == AS_BF16;
@@ -895,38 +981,36 @@ static AttendPlan plan_of(const as_ctx *ctx, const AttendArgs &a)
         if (a.prompt_table) {
             const int64_t all = a.per * (int64_t)a.group;
             const int queries = bf16 && ctx->attend_shape != 1 && (ctx->attend_shape == 2 || all >= 32) ? 128 : 16;
-            const int32_t tiles = (int32_t)((all + queries - 1) / queries);
-            add(kAttendShared, queries, (a.rows + a.per - 1) / a.per * a.kv_heads * tiles, tiles, a.prompt_room);
+            add(kAttendShared, queries, (a.rows + a.per - 1) / a.per * a.kv_heads, (int32_t)((all + queries - 1) / queries), a.prompt_room);
         }
-        if (a.table) {
-            const int32_t tiles = (a.group + 15) / 16;
-            add(kAttendOwn, 16, a.rows * a.kv_heads * tiles, tiles, a.room);
-        }
+        if (a.table) add(kAttendOwn, 16, a.rows * a.kv_heads, (a.group + 15) / 16, a.room);
+    }
+    p.every = 1;
+    if (p.count == 2) {
+        const int64_t first = p.piece[0].blocks * p.piece[0].parts, second = p.piece[1].blocks * p.piece[1].parts;
+        p.every = (int32_t)(1 + second / (2 * first));
     }
     return p;
 }
 
 size_t attend_workspace(const as_ctx *ctx, const AttendArgs &a)
 {
-    const AttendPlan p = plan_of(ctx, a);
-    return p.parts < 2 ? 0 : (size_t)a.tokens * a.heads * p.parts * (sizeof(float2) + (size_t)a.dim * sizeof(float));
+    int32_t parts;
+    (void)pieces_of(ctx, a, &parts);
+    return parts < 2 ? 0 : (size_t)a.tokens * a.heads * parts * (sizeof(float2) + (size_t)a.dim * sizeof(float));
 }
 
 as_status launch_attend(as_ctx *ctx, AttendArgs a)
 {
-    const AttendPlan p = plan_of(ctx, a);
-    a.parts = p.parts;
+    const AttendPieces p = pieces_of(ctx, a, &a.parts);
     a.sums = (float *)ctx->attend_parts.ptr;
-    a.stats = (float2 *)(a.sums + (size_t)a.tokens * a.heads * p.parts * a.dim);
-    for (int i = 0; i < p.count; ++i)
-        if (p.blocks[i] > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
-    for (int i = 0; i < p.count; ++i) {
-        const dim3 grid((unsigned)p.blocks[i], (unsigned)p.piece[i].parts);
-        if (p.piece[i].queries == 128) tiles_of(ctx, a, p.piece[i], grid);
-        else if (a.dtype == AS_BF16) rows_of<uint16_t>(ctx, a, p.piece[i], grid);
-        else rows_of<float>(ctx, a, p.piece[i], grid);
-        AS_HIP_TRY(ctx, hipGetLastError());
-    }
+    a.stats = (float2 *)(a.sums + (size_t)a.tokens * a.heads * a.parts * a.dim);
+    int64_t blocks = 0;
+    for (int i = 0; i < p.count; ++i) blocks += p.piece[i].blocks * p.piece[i].parts;
+    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
+    if (a.dtype == AS_BF16) launch_pieces<uint16_t>(ctx, a, p, dim3((unsigned)blocks));
+    else launch_pieces<float>(ctx, a, p, dim3((unsigned)blocks));
+    AS_HIP_TRY(ctx, hipGetLastError());
     if (a.parts > 1) {
         const dim3 grid((unsigned)((a.tokens * a.heads + 3) / 4));
         if (a.dtype == AS_BF16) hipLaunchKernelGGL(attend_join_kernel<uint16_t>, grid, dim3(256), 0, ctx->stream, a);
@@ -978,7 +1062,7 @@ __global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void
 as_status launch_cache_add(as_ctx *ctx, const AttendArgs &a, const void *k, int64_t ldk, const void *v, int64_t ldv)
 {
     const int32_t esz = a.dtype == AS_BF16 ? 2 : 4, pieces = 2 * a.kv_heads * (a.dim * esz / 16);
-    int32_t each = 2048 / pieces;
+    int32_t each = 256 / pieces;
     each = each < 1 ? 1 : each > 64 ? 64 : each;
     const int64_t blocks = a.offsets ? a.tokens / each + a.rows : (a.tokens + each - 1) / each;
     if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more tokens than one launch takes");

@@ -389,11 +389,16 @@ struct AttendArgs {
     int32_t parts;
 };
 enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
-struct AttendPiece {             // one launch: which keys and queries
+struct AttendPiece {             // one kind of work: which keys and queries
     int mode, queries;           // queries: of a block
-    int32_t tiles;               // of queries, of a row or prompt
+    int64_t blocks;              // (of each part)
+    int32_t tiles;               // blocks after each other that read the same keys
     int32_t part0, parts;        // the parts that it leaves
     int32_t least;               // tiles of keys that a part takes at least
+};
+struct AttendPieces {            // of one launch
+    AttendPiece piece[2];
+    int32_t count, every;
 };
 constexpr int32_t kAttendMostParts = 32;
 
