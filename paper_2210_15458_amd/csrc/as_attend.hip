@@ -536,7 +536,26 @@ template <int DP> struct TileForm {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void glb_void;
+
+// 16 bytes a lane from memory to LDS, lane after lane from `to` on (the same for the wave).  By hand, since the compiler would wait
+// for the tile that is on its way before each read of the one that is there: it takes them for one memory.  The instruction
+// writes no register; its end is waited for at the top of the loop over tiles, and what the compiler itself counts can only
+// come out as a longer wait.
+__device__ __forceinline__ void fetch_lds(const char *base, int32_t offset, unsigned char *to)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_void *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void fetch_lds(const char *from, unsigned char *to)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_void *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+}
+// What the wave has asked for has landed, what it has read of LDS is there, and so with the block's other waves.
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
 template <int DP> struct TilesShared {
     __attribute__((aligned(1024))) unsigned char smem[TileForm<DP>::kLds];
@@ -637,10 +656,13 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
             const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
             const int32_t ko = piece_of(F::key_place(row)), vo = piece_of(F::value_place(row));
             unsigned char *const to = smem + buffer * F::kBytes + (4 * i + wave) * 1024;
-            if (FULL || ko < bytes)
-                __builtin_amdgcn_global_load_lds((glb_void *)((const char *)a.k + off + (in_rows + ko)), (lds_void *)to, 16, 0, 0);
-            if (FULL || vo < bytes)
-                __builtin_amdgcn_global_load_lds((glb_void *)((const char *)a.v + off + (in_rows + vo)), (lds_void *)(to + 2 * F::kBytes), 16, 0, 0);
+            if constexpr (BYPAGE) {
+                if (FULL || ko < bytes) fetch_lds((const char *)a.k + off, in_rows + ko, to);
+                if (FULL || vo < bytes) fetch_lds((const char *)a.v + off, in_rows + vo, to + 2 * F::kBytes);
+            } else {
+                if (FULL || ko < bytes) fetch_lds((const char *)a.k + off + ko, to);
+                if (FULL || vo < bytes) fetch_lds((const char *)a.v + off + vo, to + 2 * F::kBytes);
+            }
         }
     };
 
@@ -659,8 +681,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     for (int32_t t = keys.first; t < keys.last; ++t) {
         const int buffer = (t - keys.first) & 1;
         const int32_t base = keys.base(t, BN);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
+        tile_barrier();
         if (t + 1 < keys.last) {
             fetch(t + 1, buffer ^ 1);
             find_pages(t + 2);
@@ -684,8 +705,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
                     }
                 }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
+            __syncthreads();
         }
         if (base > wave_hi) continue;                  // (the last tiles of a prompt's diagonal, for its first queries; no queries)
 
@@ -1062,7 +1082,7 @@ __global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void
 as_status launch_cache_add(as_ctx *ctx, const AttendArgs &a, const void *k, int64_t ldk, const void *v, int64_t ldv)
 {
     const int32_t esz = a.dtype == AS_BF16 ? 2 : 4, pieces = 2 * a.kv_heads * (a.dim * esz / 16);
-    int32_t each = 256 / pieces;
+    int32_t each = (a.offsets ? 2048 : 256) / pieces;
     each = each < 1 ? 1 : each > 64 ? 64 : each;
     const int64_t blocks = a.offsets ? a.tokens / each + a.rows : (a.tokens + each - 1) / each;
     if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more tokens than one launch takes");
