@@ -606,7 +606,8 @@ as_status as_history_add(as_ctx *ctx, uint32_t *seen, int64_t seen_ld, int32_t *
  * vocabulary and logits dtype.
  *
  *   k, v       DEVICE [pages, kv_heads, page_size, head_dim], dtype, a page page_ld
- *              elements behind the one before; both on 16 bytes, and so each page
+ *              elements (less than 4 GiB) behind the one before; both on 16 bytes, and so
+ *              each page
  *   page_size  tokens of a page: a power of two, at most AS_MAX_PAGE.  From 16 on
  *              the attention runs faster
  *   head_dim   a multiple of 8, at most AS_MAX_HEAD_DIM.  64, 128 and 256 run a

@@ -1252,7 +1252,8 @@ static as_status check_cache(as_ctx *ctx, const as_cache *c, const as_sequences 
         return fail(ctx, AS_ERR_INVALID_ARG, "head_dim must be a multiple of 8 in [8, AS_MAX_HEAD_DIM]");
     if (c->kv_heads < 1 || c->kv_heads > AS_MAX_HEADS) return fail(ctx, AS_ERR_INVALID_ARG, "kv_heads outside [1, AS_MAX_HEADS]");
     const int64_t esz = c->dtype == AS_BF16 ? 2 : 4, page = (int64_t)c->kv_heads * c->page_size * c->head_dim;
-    if (c->page_ld < page || c->page_ld > (int64_t)1 << 40) return fail(ctx, AS_ERR_INVALID_ARG, "page_ld is smaller than a page, or larger than 2^40");
+    if (c->page_ld < page || c->page_ld >= ((int64_t)1 << 32) / esz)
+        return fail(ctx, AS_ERR_INVALID_ARG, "page_ld is smaller than a page, or 4 GiB and more");
     if (!all_aligned(16, {c->k, c->v}) || c->page_ld * esz % 16 != 0)
         return fail(ctx, AS_ERR_INVALID_ARG, "k, v and their pages must lie on 16 bytes");
     if (s->table && (!s->lens || s->table_ld < 1)) return fail(ctx, AS_ERR_INVALID_ARG, "table needs lens and table_ld >= 1");
@@ -1264,7 +1265,7 @@ static as_status check_cache(as_ctx *ctx, const as_cache *c, const as_sequences 
     if (!all_aligned(4, {s->table, s->prompt_table}) || !all_aligned(4, {s->table ? s->lens : nullptr, s->prompt_table ? s->prompt_lens : nullptr}))
         return fail(ctx, AS_ERR_INVALID_ARG, "table, lens, prompt_table or prompt_lens is not aligned to its element type");
     *a = AttendArgs{};
-    a->k = c->k; a->v = c->v; a->pages = c->pages; a->page_bytes = c->page_ld * esz; a->kv_heads = c->kv_heads; a->dim = c->head_dim;
+    a->k = c->k; a->v = c->v; a->pages = (int32_t)c->pages; a->page_bytes = (uint32_t)(c->page_ld * esz); a->kv_heads = c->kv_heads; a->dim = c->head_dim;
     a->dtype = c->dtype;
     while ((1 << a->page_shift) < c->page_size) ++a->page_shift;
     a->rows = rows; a->tokens = rows; a->finished = s->finished;

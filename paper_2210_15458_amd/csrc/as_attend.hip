@@ -174,8 +174,8 @@ __device__ __forceinline__ Keys keys_of(const AttendArgs &a, const Work &w, int3
 __device__ __forceinline__ const char *token_at(const void *cache, const AttendArgs &a, const Work &w, int32_t t, int32_t esz)
 {
     int32_t page = w.table[t >> a.page_shift];
-    page = page < 0 ? 0 : page < a.pages ? page : (int32_t)a.pages - 1;
-    return (const char *)cache + (int64_t)page * a.page_bytes +
+    page = page < 0 ? 0 : page < a.pages ? page : a.pages - 1;
+    return (const char *)cache + (uint64_t)(uint32_t)page * a.page_bytes +
            (((int64_t)w.head << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * (int64_t)(a.dim * esz);
 }
 
@@ -217,6 +217,7 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Work &
                 const float y = d < d1 ? widen(row[d]) : 0.f;
                 const bool is = (__builtin_bit_cast(uint32_t, y) & 0x7f800000u) == 0x7f800000u;
                 if (!__any(is)) continue;
+#pragma unroll 1
                 for (int q = 0; q < QUERIES; ++q)
                     if (keys.seen(x, __builtin_amdgcn_readlane(at, q)) && is) sums[q * stride + d - d0] += y;
             }
@@ -307,8 +308,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             for (int s = 0; s < kSub; ++s) {
                 const int32_t first = base + 16 * s, there = first < keys.n ? first : base;
                 int32_t page = scalar_load(w.table + (there >> a.page_shift));
-                page = page < 0 ? 0 : page < a.pages ? page : (int32_t)a.pages - 1;
-                const int64_t off = (int64_t)page * a.page_bytes +
+                page = page < 0 ? 0 : page < a.pages ? page : a.pages - 1;
+                const int64_t off = (uint64_t)(uint32_t)page * a.page_bytes +
                                     (((int64_t)w.head << a.page_shift) + (there & ((1 << a.page_shift) - 1))) * (int64_t)bytes;
                 kp[s] = (const char *)a.k + off;
                 vp[s] = (const char *)a.v + off;
@@ -541,14 +542,18 @@ typedef __attribute__((address_space(3))) void lds_void;
 // for the tile that is on its way before each read of the one that is there: it takes them for one memory.  The instruction
 // writes no register; its end is waited for at the top of the loop over tiles, and what the compiler itself counts can only
 // come out as a longer wait.
+template <int BEHIND>             // bytes further on, there and here
 __device__ __forceinline__ void fetch_lds(const char *base, int32_t offset, unsigned char *to)
 {
-    const uint32_t at = (uint32_t)(uintptr_t)(lds_void *)to;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void *)to);
+    const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(uintptr_t)base),
+                   high = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)((uintptr_t)base >> 32));
+    base = (const char *)(low | high << 32);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(at), "v"(offset), "s"(base), "n"(BEHIND) : "memory");
 }
 __device__ __forceinline__ void fetch_lds(const char *from, unsigned char *to)
 {
-    const uint32_t at = (uint32_t)(uintptr_t)(lds_void *)to;
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void *)to);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
 }
 // What the wave has asked for has landed, what it has read of LDS is there, and so with the block's other waves.
@@ -621,47 +626,61 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     if (lo > hi) lo = hi;
     const Keys keys = keys_of(a, w, lo, hi, BN, part, piece.parts, piece.least);
 
-    // what a lane fetches: of each of its wave's kLoads KiB of a tile 16 bytes, which land in its place
-    const int row0 = wave * F::kRowsEach + lane / kPieces;            // (load i: 4 i kRowsEach further on)
-    auto piece_of = [&](int place) __attribute__((always_inline)) { return ((lane % kPieces) ^ place) * 16; };
-    int32_t page[kLoads];                              // of the tile to be fetched next
-    auto find_pages = [&](int32_t t) __attribute__((always_inline)) {
-        if (t >= keys.last) return;
-        const int32_t base = keys.base(t, BN);
+    // What a wave fetches of a tile: BN / 4 rows after each other (all in one page, of pages of 16 tokens and more), kLoads KiB, of which
+    // a lane takes 16 bytes each, such that they land in their place.
+    constexpr int kWaveRows = BN / 4;
+    const int32_t row0 = wave * kWaveRows + lane / kPieces;           // (load i: i kRowsEach further on)
+    int32_t key_off[kLoads], value_off[kLoads];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if constexpr (BYPAGE) {
-                const int32_t first = base + (4 * i + wave) * F::kRowsEach, there = first < keys.n ? first : base;
-                page[i] = scalar_load(w.table + (there >> a.page_shift));
-            } else {
-                const int32_t x = base + row0 + 4 * i * F::kRowsEach;
-                page[i] = w.table[(x < keys.n ? x : keys.n - 1) >> a.page_shift];
-            }
-            page[i] = page[i] < 0 ? 0 : page[i] < a.pages ? page[i] : (int32_t)a.pages - 1;
-        }
+    for (int i = 0; i < kLoads; ++i) {
+        const int32_t row = row0 + i * F::kRowsEach;
+        // (full rows: load i's KiB lies i KiB behind the first both in memory and in LDS, which the instruction adds)
+        const int32_t in_rows = BYPAGE ? (lane / kPieces + (FULL ? 0 : i * F::kRowsEach)) * bytes : 0;
+        key_off[i] = in_rows + ((lane % kPieces) ^ F::key_place(row)) * 16;
+        value_off[i] = in_rows + ((lane % kPieces) ^ F::value_place(row)) * 16;
+    }
+    const int32_t last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0, slots = (1 << a.page_shift) - 1;
+    const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
+    const char *const values_at = (const char *)a.v + ((int64_t)w.head << a.page_shift) * bytes;
+    struct Pages {
+        int32_t page[BYPAGE ? 1 : kLoads];
     };
-    auto fetch = [&](int32_t t, int buffer) __attribute__((always_inline)) {
-        const int32_t base = keys.base(t, BN), mask = (1 << a.page_shift) - 1;
+    auto find_pages = [&](int32_t base) __attribute__((always_inline)) {
+        Pages p;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int64_t off;
-            if constexpr (BYPAGE) {
-                const int32_t first = base + (4 * i + wave) * F::kRowsEach, there = first < keys.n ? first : base;
-                off = (int64_t)page[i] * a.page_bytes + (((int64_t)w.head << a.page_shift) + (there & mask)) * (int64_t)bytes;
+        for (int i = 0; i < (BYPAGE ? 1 : kLoads); ++i) {
+            const int32_t x = (base + (BYPAGE ? wave * kWaveRows : row0 + i * F::kRowsEach)) >> a.page_shift;
+            if constexpr (BYPAGE) p.page[i] = scalar_load(w.table + (x < last_page ? x : last_page));
+            else p.page[i] = w.table[x < last_page ? x : last_page];
+        }
+        return p;
+    };
+    // keys (to LDS buffer 0 or 1) or values (2 or 3) of the tile
+    auto fetch = [&](int32_t base, const Pages &p, int buffer) __attribute__((always_inline)) {
+        unsigned char *const to = smem + buffer * F::kBytes + wave * (kWaveRows * kRow);
+        const char *const from = buffer < 2 ? keys_at : values_at;
+        const int32_t *const off = buffer < 2 ? key_off : value_off;
+        if constexpr (BYPAGE) {
+            int32_t page = p.page[0] < 0 ? 0 : p.page[0];
+            page = page < a.pages ? page : a.pages - 1;
+            const char *const at = from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((base + wave * kWaveRows) & slots) * bytes));
+            if constexpr (FULL) {
+                fetch_lds<0>(at, off[0], to);
+                if constexpr (kLoads > 1) fetch_lds<1024>(at, off[1], to);
+                if constexpr (kLoads > 2) fetch_lds<2048>(at, off[2], to);
+                if constexpr (kLoads > 3) fetch_lds<3072>(at, off[3], to);
             } else {
-                const int32_t x = base + row0 + 4 * i * F::kRowsEach, there = x < keys.n ? x : keys.n - 1;
-                off = (int64_t)page[i] * a.page_bytes + (((int64_t)w.head << a.page_shift) + (there & mask)) * (int64_t)bytes;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    if (off[i] - (lane / kPieces + i * F::kRowsEach) * bytes < bytes) fetch_lds<0>(at, off[i], to + i * 1024);
             }
-            const int row = row0 + 4 * i * F::kRowsEach;
-            const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
-            const int32_t ko = piece_of(F::key_place(row)), vo = piece_of(F::value_place(row));
-            unsigned char *const to = smem + buffer * F::kBytes + (4 * i + wave) * 1024;
-            if constexpr (BYPAGE) {
-                if (FULL || ko < bytes) fetch_lds((const char *)a.k + off, in_rows + ko, to);
-                if (FULL || vo < bytes) fetch_lds((const char *)a.v + off, in_rows + vo, to + 2 * F::kBytes);
-            } else {
-                if (FULL || ko < bytes) fetch_lds((const char *)a.k + off + ko, to);
-                if (FULL || vo < bytes) fetch_lds((const char *)a.v + off + vo, to + 2 * F::kBytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int32_t x = base + row0 + i * F::kRowsEach, there = x < keys.n ? x : keys.n - 1;
+                int32_t page = p.page[i] < 0 ? 0 : p.page[i];
+                page = page < a.pages ? page : a.pages - 1;
+                if (off[i] < bytes) fetch_lds(from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)((there & slots) * bytes + off[i])), to + i * 1024);
             }
         }
     };
@@ -672,22 +691,97 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float m = kNone, l = 0.f;
-    if (keys.first < keys.last) {
-        find_pages(keys.first);
-        fetch(keys.first, 0);
-        find_pages(keys.first + 1);
-    }
-#pragma unroll 1
-    for (int32_t t = keys.first; t < keys.last; ++t) {
-        const int buffer = (t - keys.first) & 1;
-        const int32_t base = keys.base(t, BN);
-        tile_barrier();
-        if (t + 1 < keys.last) {
-            fetch(t + 1, buffer ^ 1);
-            find_pages(t + 2);
+    typedef f32x16 Scores[BN / 32];
+    const int kx = (half ^ F::key_place(mine)) * 16;
+    const int32_t vrow = 4 * half + (lane & 15) / 4;
+    // a tile that every query of the wave sees whole, of the block
+    const int32_t wave_whole = (keys.n < wave_lo + 1 ? keys.n : wave_lo + 1) - BN, block_whole = (keys.n < lo + 1 ? keys.n : lo + 1) - BN;
+    const int32_t wave_from = a.window > 0 ? wave_hi - a.window : -1, block_from = a.window > 0 ? hi - a.window : -1;
+
+    // The pieces of a tile's work, in the order that they are to be issued in: the products of scores a key fragment ahead of
+    // their operands, with a share of another tile's weights under each.
+    constexpr int kScoreSteps = BN / 32 * (DP / 16), kValueSteps = BN / 16 * (DP / 32), kPairs = BN / 4;
+    auto key_fragment = [&](const unsigned char *krow, int j) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8 *>(krow + j % (BN / 32) * 32 * kRow + ((j / (BN / 32) * 32) ^ kx));
+    };
+    auto value_fragment = [&](const unsigned char *vrows, int j) __attribute__((always_inline)) {
+        const int i = j / (DP / 32), d = j % (DP / 32), c = (d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ F::value_place(vrow);
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(vrows + i * 16 * kRow + c * 16));
+        const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(vrows + (i * 16 + 8) * kRow + c * 16));
+        return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // two of a lane's weights, rounded to bf16 for the second product; l adds up the rounded ones, so that they come to 1 all the same
+    auto weigh = [&](const Scores &s, int j, float ref) __attribute__((always_inline)) -> uint32_t {
+        const float x = s[j >> 3][j % 8 * 2], y = s[j >> 3][j % 8 * 2 + 1];
+        const uint32_t w2 = weights2(__builtin_amdgcn_exp2f(fmaf(x, scale, -ref)), __builtin_amdgcn_exp2f(fmaf(y, scale, -ref)));
+        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w2), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+        return w2;
+    };
+    auto score = [&](const unsigned char *ks, Scores &s, auto under) __attribute__((always_inline)) {
+        const unsigned char *const krow = ks + mine * kRow;
+        bf16x8 k[3] = {key_fragment(krow, 0), key_fragment(krow, 1), key_fragment(krow, 2)};
+#pragma unroll
+        for (int j = 0; j < kScoreSteps; ++j) {
+            const int b = j % (BN / 32), i = j / (BN / 32);
+            if (i == 0) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+            }
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j % 3], __builtin_bit_cast(bf16x8, q[i]), s[b], 0, 0, 0);
+            if (j + 3 < kScoreSteps) k[j % 3] = key_fragment(krow, j + 3);
+            under(j);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        unsigned char *const ks = smem + buffer * F::kBytes, *const vs = ks + 2 * F::kBytes;
-        if (!keys.whole(base, BN)) {
+    };
+    auto hide = [&](int32_t base, Scores &s) __attribute__((always_inline)) {
+        if (base <= wave_whole && (base > wave_from || base + BN <= keys.sinks)) return;
+        const int32_t first = base + 4 * half, upto = (at < keys.n ? at : keys.n - 1) - first;      // (of the tile's tokens, as the lane has them)
+        if (a.window > 0) {
+            const int32_t from = at - a.window - first, sinks = keys.sinks - first;
+#pragma unroll
+            for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int x = b * 32 + 8 * (r >> 2) + (r & 3);
+                    const float y = x < sinks ? s[b][r] : kNone, z = x > from ? s[b][r] : y;
+                    s[b][r] = x <= upto ? z : kNone;
+                }
+        } else {
+#pragma unroll
+            for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + 8 * (r >> 2) + (r & 3) <= upto ? s[b][r] : kNone;
+        }
+    };
+    auto add_values = [&](const unsigned char *vs, const u32x4 (&pw)[BN / 16]) __attribute__((always_inline)) {
+        const unsigned char *const vrows = vs + vrow * kRow + (lane & 1) * 8;
+        bf16x8 v[3] = {value_fragment(vrows, 0), value_fragment(vrows, 1), value_fragment(vrows, 2)};
+#pragma unroll
+        for (int j = 0; j < kValueSteps; ++j) {
+            const int i = j / (DP / 32), d = j % (DP / 32);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[j % 3], __builtin_bit_cast(bf16x8, pw[i]), o[d], 0, 0, 0);
+            if (j + 3 < kValueSteps) v[j % 3] = value_fragment(vrows, j + 3);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // One tile: its weights and their product with its values, under it the next tile's scores; the tile after that one's keys and
+    // the next one's values are asked for.
+    Pages ahead;                                       // of the next tile ...
+    int32_t next_base = 0, after_base = 0;             // ... and where it and the one after it start
+    auto step = [&](int32_t t, int32_t base, int buffer, Scores &now, Scores &next) __attribute__((always_inline)) {
+        tile_barrier();
+        const bool more = t + 1 < keys.last;
+        if (more) {
+            next_base = keys.base(t + 1, BN);
+            fetch(next_base, ahead, 2 + (buffer ^ 1));
+        }
+        if (t + 2 < keys.last) {
+            after_base = keys.base(t + 2, BN);
+            ahead = find_pages(after_base);
+            fetch(after_base, ahead, buffer);
+        }
+        unsigned char *const vs = smem + (2 + buffer) * F::kBytes;
+        if (!(base <= block_whole && (base > block_from || base + BN <= keys.sinks))) {
             // what no query sees may be anything, and 0 * NaN is NaN; what is no number and seen by some alone is added at the end
             for (int i = threadIdx.x; i < BN * kPieces; i += 256) {
                 u32x4 *const p = reinterpret_cast<u32x4 *>(vs) + i;
@@ -707,66 +801,60 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
             }
             __syncthreads();
         }
-        if (base > wave_hi) continue;                  // (the last tiles of a prompt's diagonal, for its first queries; no queries)
-
-        // scores
-        f32x16 s[BN / 32];
-        const unsigned char *const krow = ks + mine * kRow;
-        const int kx = (half ^ F::key_place(mine)) * 16;
-#pragma unroll
-        for (int b = 0; b < BN / 32; ++b) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(krow + b * 32 * kRow + ((i * 32) ^ kx));
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, __builtin_bit_cast(bf16x8, q[i]), s[b], 0, 0, 0);
-            }
-        }
-        if (!(base + BN <= keys.n && base + BN - 1 <= wave_lo && (a.window <= 0 || base > wave_hi - a.window || base + BN <= keys.sinks))) {
-#pragma unroll
-            for (int b = 0; b < BN / 32; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[b][r] = keys.seen(base + b * 32 + 8 * (r >> 2) + 4 * half + (r & 3), at) ? s[b][r] : kNone;
-        }
+        if (wave_hi < 0) return;                       // (no queries)
         float top = kNone;
 #pragma unroll
         for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, now[b][r]);
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
         top = top == kNone ? kNone : top * scale;
         if (__any(top > m + 8.f)) {
-            const float now = fmaxf(top, m);
-            const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
+            const float up = fmaxf(top, m);
+            const float by = up == kNone ? 1.f : __builtin_amdgcn_exp2f(m - up);
+            m = up;
             l *= by;
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) o[i] *= by;
         }
         const float ref = m == kNone ? 0.f : m;
-        // weights, rounded to bf16 for the second product; l adds up the rounded ones, so that they come to 1 all the same
+        u32x4 pw[BN / 16];
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            score(smem + (buffer ^ 1) * F::kBytes, next, [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < BN / 16; ++i) {
-            u32x4 pw;
+                for (int e = j * kPairs / kScoreSteps; e < (j + 1) * kPairs / kScoreSteps; ++e) pw[e / 4][e % 4] = weigh(now, e, ref);
+            });
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x = s[i >> 1][(i & 1) * 8 + 2 * e], y = s[i >> 1][(i & 1) * 8 + 2 * e + 1];
-                pw[e] = weights2(__builtin_amdgcn_exp2f(fmaf(x, scale, -ref)), __builtin_amdgcn_exp2f(fmaf(y, scale, -ref)));
-                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)pw[e]), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
-            }
-            const int vrow = 4 * half + (lane & 15) / 4;
-            const unsigned char *const from = vs + vrow * kRow + (lane & 1) * 8;
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d) {
-                const int c = (d * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ F::value_place(vrow);
-                const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(from + i * 16 * kRow + c * 16));
-                const bf16x4 v1 =
-                    __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(from + (i * 16 + 8) * kRow + c * 16));
-                const bf16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pw), o[d], 0, 0, 0);
-            }
+            for (int e = 0; e < kPairs; ++e) pw[e / 4][e % 4] = weigh(now, e, ref);
+        }
+        add_values(vs, pw);
+        if (more) hide(next_base, next);
+    };
+    if (keys.first < keys.last) {
+        const int32_t base = keys.base(keys.first, BN);
+        ahead = find_pages(base);
+        fetch(base, ahead, 0);
+        fetch(base, ahead, 2);
+        if (keys.first + 1 < keys.last) {
+            next_base = keys.base(keys.first + 1, BN);
+            ahead = find_pages(next_base);
+        }
+        tile_barrier();
+        if (keys.first + 1 < keys.last) fetch(next_base, ahead, 1);
+        Scores one, two;
+        score(smem, one, [](int) {});
+        hide(base, one);
+        int32_t t = keys.first, at_base = base;
+#pragma unroll 1
+        for (;;) {
+            step(t, at_base, 0, one, two);
+            if (++t >= keys.last) break;
+            at_base = next_base;
+            step(t, at_base, 1, two, one);
+            if (++t >= keys.last) break;
+            at_base = next_base;
         }
     }
 
@@ -1072,7 +1160,7 @@ __global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void
         const bool value = x >= pieces / 2;
         const int32_t y = value ? x - pieces / 2 : x, head = y / per_head, at = (y - head * per_head) * 16;
         const char *const source = (const char *)(value ? v : k) + token * (value ? ldv : ldk) * esz + (int64_t)y * 16;
-        char *const target = (char *)const_cast<void *>(value ? a.v : a.k) + (int64_t)page * a.page_bytes +
+        char *const target = (char *)const_cast<void *>(value ? a.v : a.k) + (uint64_t)(uint32_t)page * a.page_bytes +
                              (((int64_t)head << a.page_shift) + (pos & ((1 << a.page_shift) - 1))) * (int64_t)(a.dim * esz) + at;
         const u32x4_any in = *reinterpret_cast<const u32x4_any *>(source);
         *reinterpret_cast<u32x4 *>(target) = u32x4{in[0], in[1], in[2], in[3]};

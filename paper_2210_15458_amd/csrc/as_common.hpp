@@ -362,7 +362,8 @@ struct HistoryArgs {
 
 struct AttendArgs {
     const void *k, *v;           // [pages, kv_heads, page, dim]
-    int64_t pages, page_bytes;   // (from page to page)
+    int32_t pages;
+    uint32_t page_bytes;         // from page to page
     int32_t page_shift, kv_heads, dim;
     as_dtype dtype;
     const void *q;               // [tokens, heads, dim], rows ldq apart
