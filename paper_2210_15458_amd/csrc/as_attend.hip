@@ -35,13 +35,17 @@ __device__ __forceinline__ int64_t offset_at(const AttendArgs &a, int64_t s)
     const int64_t o = a.offsets[s];
     return o < 0 ? 0 : o > a.tokens ? a.tokens : o;
 }
-// The last sequence whose first slot is at most `slot` (rows 0: whose first token is); 64 of them looked at at once.
-__device__ __forceinline__ int64_t find_sequence(const AttendArgs &a, int64_t slot, int32_t group, int32_t rows)
+// The last sequence whose first slot is at most `slot` (ROWS 0: whose first token is); 64 of them looked at at once.
+template <int ROWS> __device__ __forceinline__ int64_t find_sequence(const AttendArgs &a, int64_t slot, uint32_t group, uint32_t rows = ROWS)
 {
     int64_t lo = 0, hi = a.rows;                       // the answer is in [lo, hi)
     while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) / 64, s = lo + (lane_id() + 1) * step;
-        const bool behind = s < hi && (rows ? offset_at(a, s) * group / rows + s : offset_at(a, s)) <= slot;
+        const int64_t step = (hi - lo + 63) >> 6, s = lo + (lane_id() + 1) * step;
+        bool behind = false;
+        if (s < hi) {
+            const uint64_t o = offset_at(a, s);
+            behind = (int64_t)(ROWS > 0 ? o * group / rows + s : o) <= slot;
+        }
         const int n = __popcll(__ballot(behind));      // (monotone: the first n lanes)
         const int64_t next = lo + n * step;
         hi = next + step < hi ? next + step : hi;
@@ -68,55 +72,59 @@ __device__ __forceinline__ int32_t length_of(const int32_t *lens, int64_t i, int
     return n < 0 ? 0 : n > room ? room : n;
 }
 
-// Query `mine` (0 .. rows-1) of tile blockIdx.x.  False where the block has nothing to do.
-__device__ __forceinline__ bool find_work(const AttendArgs &a, int32_t mode, int32_t rows, int32_t tiles, int32_t mine, int64_t item, Work &w)
+// Query `mine` of the ROWS of an item.  False where the block has nothing to do.  (The launch sees to it that a sequence's queries
+// times the heads of a group fit 32 bits.)
+template <int ROWS>
+__device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece &piece, uint32_t mine, uint32_t item, Work &w)
 {
-    const int32_t G = a.group;
-    if (mode == kAttendRagged) {
-        const int64_t slot = item / a.kv_heads;
+    const uint32_t G = a.group;
+    // x / G for x < G + 128
+    auto by_group = [&](uint32_t x) __attribute__((always_inline)) { return x * a.group_inverse >> 24; };
+    if (piece.mode == kAttendRagged) {
+        const uint32_t slot = item / (uint32_t)a.kv_heads;
         w.head = (int32_t)(item - slot * a.kv_heads);
-        const int64_t s = find_sequence(a, slot, G, rows);
+        const int64_t s = find_sequence<ROWS>(a, slot, G);
         const int64_t from = offset_at(a, s), to = offset_at(a, s + 1);
-        const int64_t first = (slot - s - from * G / rows) * rows;      // the tile's first row in its sequence
-        const int64_t all = (to - from) * G;
-        if (first < 0 || first >= all || (a.finished && a.finished[s])) return false;      // (below 0: offsets that fall)
         const int32_t len = length_of(a.lens, s, a.room);
+        const int64_t first = ((int64_t)slot - s - (int64_t)((uint64_t)from * G / ROWS)) * ROWS;      // the tile's first row in its sequence
+        const int64_t all = (to - from) * G;
+        // (below 0: offsets that fall)
+        if (first < 0 || first >= all || (a.finished && a.finished[s])) return false;
         w.table = a.table + s * a.table_ld;
         w.n = len;
         w.key0 = 0;
-        const int64_t m = first + mine;
-        w.valid = m < all;
-        const int32_t i = (int32_t)((w.valid ? m : all - 1) / G);
-        w.token = from + i;
-        w.qhead = w.head * G + (int32_t)(m - (int64_t)i * G);
-        w.at = len - (int32_t)(to - from) + i;
+        const uint32_t first_token = (uint32_t)first / G, rest = (uint32_t)first - first_token * G, left = (uint32_t)(all - first);
+        w.valid = mine < left;
+        const uint32_t x = rest + (w.valid ? mine : left - 1), i = by_group(x);
+        w.token = from + first_token + i;
+        w.qhead = (int32_t)(w.head * G + x - i * G);
+        w.at = len - (int32_t)(to - from) + (int32_t)(first_token + i);
         return true;
     }
-    const int32_t tile = (int32_t)(item % tiles);
-    const int64_t rest = item / tiles;
-    w.head = (int32_t)(rest % a.kv_heads);
-    const int64_t p = rest / a.kv_heads;                // row or prompt
-    if (mode == kAttendOwn) {
+    const uint32_t group = item / (uint32_t)piece.tiles, tile = item - group * piece.tiles;
+    const uint32_t p = group / (uint32_t)a.kv_heads;    // row or prompt
+    w.head = (int32_t)(group - p * a.kv_heads);
+    if (piece.mode == kAttendOwn) {
         if (a.finished && a.finished[p]) return false;
-        const int32_t g = tile * rows + mine;
+        const uint32_t g = tile * ROWS + mine;
         w.valid = g < G;
         w.token = p;
-        w.qhead = w.head * G + g;
+        w.qhead = (int32_t)(w.head * G + g);
         w.table = a.table + p * a.table_ld;
         w.n = length_of(a.lens, p, a.room);
-        w.key0 = a.prompt_table ? length_of(a.prompt_lens, p / a.per, a.prompt_room) : 0;
+        w.key0 = a.prompt_table ? length_of(a.prompt_lens, p / (uint32_t)a.per, a.prompt_room) : 0;
         w.at = w.n - 1;
         return true;
     }
     w.table = a.prompt_table + p * a.prompt_table_ld;
     w.n = length_of(a.prompt_lens, p, a.prompt_room);
     w.key0 = 0;
-    const int64_t m = (int64_t)tile * rows + mine;
-    const int64_t c = m / G, row = p * a.per + c;
-    w.valid = c < a.per && row < a.rows;
+    const uint32_t first = tile * ROWS, first_row = first / G, x = first - first_row * G + mine, c = by_group(x);
+    const int64_t row = (int64_t)p * a.per + first_row + c;
+    w.valid = first_row + c < (uint32_t)a.per && row < a.rows;
     if (w.valid && a.finished && a.finished[row]) w.valid = false;
     w.token = row;
-    w.qhead = w.head * G + (int32_t)(m - c * G);
+    w.qhead = (int32_t)(w.head * G + x - c * G);
     int32_t own = 0;
     if (w.valid && a.table) {
         own = a.lens[row];
@@ -250,7 +258,7 @@ template <class T, int DP> struct RowsShared {
 };
 
 template <class T, int DP, bool FULL, bool BYPAGE>
-__device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPiece &piece, int64_t item, int32_t part, RowsShared<T, DP> &shared)
+__device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, RowsShared<T, DP> &shared)
 {
     typedef AttendForm<T, DP> F;
     constexpr int kSub = F::kSub, kKey = F::kKey, kVBytes = F::kVBytes, kChunks = F::kChunks, kEach = F::kEach, BN = 16 * kSub;
@@ -263,7 +271,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * (int32_t)sizeof(T);
     Work w;
-    if (!find_work(a, piece.mode, 16, piece.tiles, mine, item, w)) return;
+    if (!find_work<16>(a, piece, mine, item, w)) return;
     int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = w.valid ? w.at : -1;
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
@@ -569,7 +577,7 @@ template <int DP> struct TilesShared {
 };
 
 template <int DP, bool FULL, bool BYPAGE>
-__device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPiece &piece, int64_t item, int32_t part, TilesShared<DP> &shared)
+__device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, TilesShared<DP> &shared)
 {
     typedef TileForm<DP> F;
     constexpr int BN = F::kKeys, kLoads = F::kLoads, kPieces = F::kPieces, kStride = F::kStride, kRow = DP * 2;
@@ -581,7 +589,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * 2;
     Work w;
-    if (!find_work(a, piece.mode, F::kQueries, piece.tiles, wave * 32 + mine, item, w)) return;
+    if (!find_work<F::kQueries>(a, piece, wave * 32 + mine, item, w)) return;
     const int32_t at = w.valid ? w.at : -1;
     int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = at;
 #pragma unroll
@@ -827,7 +835,10 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
             });
         } else {
 #pragma unroll
-            for (int e = 0; e < kPairs; ++e) pw[e / 4][e % 4] = weigh(now, e, ref);
+            for (int e = 0; e < kPairs; ++e) {
+                pw[e / 4][e % 4] = weigh(now, e, ref);
+                if (e % 2) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         add_values(vs, pw);
         if (more) hide(next_base, next);
@@ -909,33 +920,39 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 
 // Which work is block b's: of a piece's items, of which `tiles` after each other read the same keys, those of a group go to one
 // XCD (blocks go round the eight), whose L2 then has the keys; of ragged queries the last first, which see most keys.
-__device__ __forceinline__ void item_of(const AttendPiece &p, int64_t b, int64_t *item, int32_t *part)
+__device__ __forceinline__ void item_of(const AttendPiece &p, uint32_t b, uint32_t *item, int32_t *part)
 {
-    const int64_t groups = p.blocks / p.tiles * p.parts, whole = groups & ~(int64_t)7;
-    if (p.mode == kAttendRagged) {
-        *part = (int32_t)(b / p.blocks);
-        *item = p.blocks - 1 - (b - *part * p.blocks);
+    if (p.parts == 1 && p.tiles == 1) {
+        *part = 0;
+        *item = p.mode == kAttendRagged ? p.blocks - 1 - b : b;
         return;
     }
-    int64_t group;
-    int32_t tile;
-    if (b < whole * p.tiles) {
-        const int64_t j = b >> 3;
-        tile = (int32_t)(j % p.tiles);
-        group = j / p.tiles * 8 + (b & 7);
-    } else {
-        tile = (int32_t)(b % p.tiles);
-        group = b / p.tiles;
+    if (p.mode == kAttendRagged) {
+        const uint32_t x = b / p.blocks;
+        *part = (int32_t)x;
+        *item = p.blocks - 1 - (b - x * p.blocks);
+        return;
     }
-    *part = (int32_t)(group / (p.blocks / p.tiles));
-    *item = (group - *part * (p.blocks / p.tiles)) * p.tiles + tile;
+    const uint32_t tiles = p.tiles, groups = p.groups, whole = (groups * p.parts & ~7u) * tiles;
+    uint32_t group, tile;
+    if (b < whole) {
+        const uint32_t j = b >> 3, g = j / tiles;
+        tile = j - g * tiles;
+        group = g * 8 + (b & 7);
+    } else {
+        group = b / tiles;
+        tile = b - group * tiles;
+    }
+    const uint32_t x = group / groups;
+    *part = (int32_t)x;
+    *item = (group - x * groups) * tiles + tile;
 }
 
 // With two pieces (what rows share, and their own) every `every`-th block is one of the first, as long as there are any.
-__device__ __forceinline__ bool first_piece(const AttendPieces &p, int64_t *b)
+__device__ __forceinline__ bool first_piece(const AttendPieces &p, uint32_t *b)
 {
     if (p.count < 2) return true;
-    const int64_t all = p.piece[0].blocks * p.piece[0].parts, turn = *b / p.every;
+    const uint32_t all = p.piece[0].blocks * p.piece[0].parts, turn = *b / p.every;
     if (turn < all && *b == turn * p.every) {
         *b = turn;
         return true;
@@ -948,7 +965,7 @@ template <class T, int DP, bool FULL, bool BYPAGE>
 __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ RowsShared<T, DP> shared;
-    int64_t b = blockIdx.x, item;
+    uint32_t b = blockIdx.x, item;
     int32_t part;
     const AttendPiece &piece = first_piece(p, &b) ? p.piece[0] : p.piece[1];
     item_of(piece, b, &item, &part);
@@ -959,7 +976,7 @@ template <int DP, bool FULL, bool BYPAGE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ TilesShared<DP> shared;
-    int64_t item;
+    uint32_t item;
     int32_t part;
     item_of(p.piece[0], blockIdx.x, &item, &part);
     attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared);
@@ -972,7 +989,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_both_kernel(Att
         TilesShared<DP> tiles;
         RowsShared<uint16_t, DP> rows;
     } shared;
-    int64_t b = blockIdx.x, item;
+    uint32_t b = blockIdx.x, item;
     int32_t part;
     if (first_piece(p, &b)) {
         item_of(p.piece[0], b, &item, &part);
@@ -995,7 +1012,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     if (token >= a.tokens) return;
     if (a.offsets) {
         if (token < offset_at(a, 0) || token >= offset_at(a, a.rows)) return;
-        if (a.finished && a.finished[find_sequence(a, token, 1, 0)]) return;
+        if (a.finished && a.finished[find_sequence<0>(a, token, 1)]) return;
     } else if (a.finished && a.finished[token]) return;
     const float2 *const stats = a.stats + i * a.parts;
     const float2 mine = lane < a.parts ? stats[lane] : float2{kNone, 0.f};
@@ -1065,10 +1082,12 @@ static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room, int64_
     return (int32_t)(n < 1 ? 1 : n > kAttendMostParts ? kAttendMostParts : n);
 }
 
-static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *parts)
+static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *parts, bool *fit)
 {
     AttendPieces p{};
     *parts = 0;
+    // (a sequence's or a prompt's queries, and the blocks, in 32 bits)
+    bool fits = a.tokens * a.group <= 0x7fffffffLL - 128 && a.per * (int64_t)a.group <= 0x7fffffffLL - 128;
     auto add = [&](int mode, int queries, int64_t groups, int32_t tiles, int64_t room) {
         AttendPiece &x = p.piece[p.count++];
         x.mode = mode;
@@ -1076,9 +1095,11 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         x.tiles = tiles;
         x.least = queries == 16 ? 8 : 4;
         x.part0 = *parts;
-        x.blocks = groups * tiles;
-        x.parts = parts_for(ctx, x.blocks, room, queries == 16 ? 256 : 512);
+        x.parts = parts_for(ctx, groups * tiles, room, queries == 16 ? 256 : 512);
         *parts += x.parts;
+        fits = fits && groups * tiles * x.parts <= 0x7fffffffLL;
+        x.groups = (uint32_t)groups;
+        x.blocks = (uint32_t)(groups * tiles);
     };
     // many queries that share a key head: by tiles of 128
     const bool bf16 = a.dtype == AS_BF16;
@@ -1095,27 +1116,32 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
     }
     p.every = 1;
     if (p.count == 2) {
-        const int64_t first = p.piece[0].blocks * p.piece[0].parts, second = p.piece[1].blocks * p.piece[1].parts;
-        p.every = (int32_t)(1 + second / (2 * first));
+        const int64_t first = (int64_t)p.piece[0].blocks * p.piece[0].parts, second = (int64_t)p.piece[1].blocks * p.piece[1].parts;
+        p.every = (uint32_t)(1 + second / (2 * first));
+        fits = fits && first + second <= 0x7fffffffLL;
     }
+    *fit = fits;
     return p;
 }
 
 size_t attend_workspace(const as_ctx *ctx, const AttendArgs &a)
 {
     int32_t parts;
-    (void)pieces_of(ctx, a, &parts);
-    return parts < 2 ? 0 : (size_t)a.tokens * a.heads * parts * (sizeof(float2) + (size_t)a.dim * sizeof(float));
+    bool fit;
+    (void)pieces_of(ctx, a, &parts, &fit);
+    return parts < 2 || !fit ? 0 : (size_t)a.tokens * a.heads * parts * (sizeof(float2) + (size_t)a.dim * sizeof(float));
 }
 
 as_status launch_attend(as_ctx *ctx, AttendArgs a)
 {
-    const AttendPieces p = pieces_of(ctx, a, &a.parts);
+    bool fit;
+    const AttendPieces p = pieces_of(ctx, a, &a.parts, &fit);
+    if (!fit) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
+    a.group_inverse = ((1u << 24) + a.group - 1) / a.group;
     a.sums = (float *)ctx->attend_parts.ptr;
     a.stats = (float2 *)(a.sums + (size_t)a.tokens * a.heads * a.parts * a.dim);
     int64_t blocks = 0;
-    for (int i = 0; i < p.count; ++i) blocks += p.piece[i].blocks * p.piece[i].parts;
-    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more queries than one launch takes");
+    for (int i = 0; i < p.count; ++i) blocks += (int64_t)p.piece[i].blocks * p.piece[i].parts;
     if (a.dtype == AS_BF16) launch_pieces<uint16_t>(ctx, a, p, dim3((unsigned)blocks));
     else launch_pieces<float>(ctx, a, p, dim3((unsigned)blocks));
     AS_HIP_TRY(ctx, hipGetLastError());
@@ -1139,7 +1165,7 @@ __global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void
     const int32_t per_head = a.dim * esz / 16, pieces = 2 * a.kv_heads * per_head;
     int64_t s = 0, from = 0, to = 0, first;
     if (a.offsets) {
-        s = find_sequence(a, blockIdx.x, 1, tokens_each);
+        s = find_sequence<1>(a, blockIdx.x, 1, tokens_each);
         from = offset_at(a, s);
         to = offset_at(a, s + 1);
         first = from + ((int64_t)blockIdx.x - s - from / tokens_each) * tokens_each;

@@ -371,6 +371,7 @@ struct AttendArgs {
     void *out;
     int64_t ldo;
     int32_t heads, group;        // group: of a key head
+    uint32_t group_inverse;      // 2^24 / group, rounded up
     float scale;                 // times log2(e)
     int32_t window, sinks;       // window <= 0: none
     int64_t rows;                // sequences
@@ -392,14 +393,15 @@ struct AttendArgs {
 enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
 struct AttendPiece {             // one kind of work: which keys and queries
     int mode, queries;           // queries: of a block
-    int64_t blocks;              // (of each part)
+    uint32_t groups, blocks;     // blocks: of each part, `tiles` a group
     int32_t tiles;               // blocks after each other that read the same keys
     int32_t part0, parts;        // the parts that it leaves
     int32_t least;               // tiles of keys that a part takes at least
 };
 struct AttendPieces {            // of one launch
     AttendPiece piece[2];
-    int32_t count, every;
+    int32_t count;
+    uint32_t every;
 };
 constexpr int32_t kAttendMostParts = 32;
 
