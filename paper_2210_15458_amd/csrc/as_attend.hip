@@ -550,14 +550,25 @@ typedef __attribute__((address_space(3))) void lds_void;
 // for the tile that is on its way before each read of the one that is there: it takes them for one memory.  The instruction
 // writes no register; its end is waited for at the top of the loop over tiles, and what the compiler itself counts can only
 // come out as a longer wait.
-template <int BEHIND>             // bytes further on, there and here
-__device__ __forceinline__ void fetch_lds(const char *base, int32_t offset, unsigned char *to)
+template <int N>                  // N KiB, each a KiB behind the one before both there and here
+__device__ __forceinline__ void fetch_lds(const char *base, const int32_t (&offset)[N], unsigned char *to)
 {
+    static_assert(N == 1 || N == 2 || N == 4, "written out for these");
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void *)to);
     const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(uintptr_t)base),
                    high = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)((uintptr_t)base >> 32));
     base = (const char *)(low | high << 32);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(at), "v"(offset), "s"(base), "n"(BEHIND) : "memory");
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(at), "s"(base), "v"(offset[0]) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024" ::"s"(at),
+                     "s"(base), "v"(offset[0]), "v"(offset[1])
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072" ::"s"(at),
+                     "s"(base), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3])
+                     : "memory");
 }
 __device__ __forceinline__ void fetch_lds(const char *from, unsigned char *to)
 {
@@ -575,6 +586,13 @@ template <int DP> struct TilesShared {
     int64_t rows_at[TileForm<DP>::kQueries];
     int32_t ends[2][4], any_odd;
 };
+
+// The other half of a wave's value beside a lane's own.
+__device__ __forceinline__ float halves_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
 
 template <int DP, bool FULL, bool BYPAGE>
 __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, TilesShared<DP> &shared)
@@ -667,20 +685,17 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     auto fetch = [&](int32_t base, const Pages &p, int buffer) __attribute__((always_inline)) {
         unsigned char *const to = smem + buffer * F::kBytes + wave * (kWaveRows * kRow);
         const char *const from = buffer < 2 ? keys_at : values_at;
-        const int32_t *const off = buffer < 2 ? key_off : value_off;
+        const int32_t(&off)[kLoads] = buffer < 2 ? key_off : value_off;
         if constexpr (BYPAGE) {
             int32_t page = p.page[0] < 0 ? 0 : p.page[0];
             page = page < a.pages ? page : a.pages - 1;
             const char *const at = from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((base + wave * kWaveRows) & slots) * bytes));
             if constexpr (FULL) {
-                fetch_lds<0>(at, off[0], to);
-                if constexpr (kLoads > 1) fetch_lds<1024>(at, off[1], to);
-                if constexpr (kLoads > 2) fetch_lds<2048>(at, off[2], to);
-                if constexpr (kLoads > 3) fetch_lds<3072>(at, off[3], to);
+                fetch_lds(at, off, to);
             } else {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
-                    if (off[i] - (lane / kPieces + i * F::kRowsEach) * bytes < bytes) fetch_lds<0>(at, off[i], to + i * 1024);
+                    if (off[i] - (lane / kPieces + i * F::kRowsEach) * bytes < bytes) fetch_lds(at, {off[i]}, to + i * 1024);
             }
         } else {
 #pragma unroll
@@ -815,7 +830,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, now[b][r]);
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        top = halves_max(top);
         top = top == kNone ? kNone : top * scale;
         if (__any(top > m + 8.f)) {
             const float up = fmaxf(top, m);
@@ -828,6 +843,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         const float ref = m == kNone ? 0.f : m;
         u32x4 pw[BN / 16];
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
         if (more) {
             score(smem + (buffer ^ 1) * F::kBytes, next, [&](int j) __attribute__((always_inline)) {
 #pragma unroll
@@ -841,6 +857,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
             }
         }
         add_values(vs, pw);
+        __builtin_amdgcn_s_setprio(0);
         if (more) hide(next_base, next);
     };
     if (keys.first < keys.last) {
