@@ -250,6 +250,15 @@ template <int DP> struct AttendForm<float, DP> {
     static constexpr int kSub = 1, kKey = DP / 16, kVBytes = 16, kChunks = DP / 64, kEach = 4;
 };
 
+// Four or eight values after each other.
+__device__ __forceinline__ void store_some(float *p, const float (&y)[4]) { *reinterpret_cast<f32x4_any *>(p) = f32x4{y[0], y[1], y[2], y[3]}; }
+__device__ __forceinline__ void store_some(uint16_t *p, const float (&y)[4])
+{
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<u32x2_any *>(p) = u32x2{weights2(y[0], y[1]), weights2(y[2], y[3])};
+}
+template <class T> __device__ __forceinline__ void store_some(T *p, const float (&y)[8]) { store8(p, y); }
+
 template <class T, int DP> struct RowsShared {
     static constexpr int kStride = DP + 4;
     __attribute__((aligned(16))) float sums[4 * 16 * kStride];
@@ -257,7 +266,7 @@ template <class T, int DP> struct RowsShared {
     int64_t rows_at[16];                               // token * heads + head of each query, -1: none
 };
 
-template <class T, int DP, bool FULL, bool BYPAGE>
+template <class T, int DP, bool FULL, bool BYPAGE, int WAVES>
 __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, RowsShared<T, DP> &shared)
 {
     typedef AttendForm<T, DP> F;
@@ -284,6 +293,22 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     if (lo_at > hi_at) lo_at = hi_at;                  // (no query)
     const Keys keys = keys_of(a, w, lo_at, hi_at, BN, part, piece.parts, piece.least);
     const int32_t at = w.valid ? w.at : -1;
+    const int32_t first = keys.first + (WAVES > 1 ? wave : 0), last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0;
+    // pages of a tile's tokens: of its sixteens, or of a token a lane; looked up a tile ahead
+    struct Pages {
+        int32_t page[BYPAGE ? kSub : 1];
+    };
+    auto find_pages = [&](int32_t base) __attribute__((always_inline)) {
+        Pages p;
+#pragma unroll
+        for (int i = 0; i < (BYPAGE ? kSub : 1); ++i) {
+            const int32_t x = (BYPAGE ? base + 16 * i : base + (lane & (BN - 1))) >> a.page_shift, there = x < last_page ? x : last_page;
+            p.page[i] = BYPAGE ? scalar_load(w.table + there) : w.table[there];
+        }
+        return p;
+    };
+    Pages ahead;
+    if (first < keys.last) ahead = find_pages(keys.base(first, BN));
 
     // the queries, zeros where there is none and past the row's end
     u32x4 q[kKey];
@@ -304,35 +329,35 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     float m = kNone, l = 0.f;
     bool odd = false;
 
+    const int32_t slots = (1 << a.page_shift) - 1;
+    const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
+    const int64_t values_behind = (const char *)a.v - (const char *)a.k;
 #pragma unroll 1
-    for (int32_t t = keys.first + wave; t < keys.last; t += 4) {
+    for (int32_t t = first; t < keys.last; t += WAVES) {
         const int32_t base = keys.base(t, BN);
         u32x4 k[kSub][kKey];
         uint32_t v[kSub * 4][kChunks][kWords];
-        const char *kp[kSub], *vp[kSub];
-        if constexpr (BYPAGE) {
-            // 16 tokens lie in one page
+        Pages now = ahead;
+        if (t + WAVES < keys.last) ahead = find_pages(keys.base(t + WAVES, BN));
 #pragma unroll
-            for (int s = 0; s < kSub; ++s) {
-                const int32_t first = base + 16 * s, there = first < keys.n ? first : base;
-                int32_t page = scalar_load(w.table + (there >> a.page_shift));
-                page = page < 0 ? 0 : page < a.pages ? page : a.pages - 1;
-                const int64_t off = (uint64_t)(uint32_t)page * a.page_bytes +
-                                    (((int64_t)w.head << a.page_shift) + (there & ((1 << a.page_shift) - 1))) * (int64_t)bytes;
-                kp[s] = (const char *)a.k + off;
-                vp[s] = (const char *)a.v + off;
-            }
+        for (int i = 0; i < (BYPAGE ? kSub : 1); ++i) {
+            now.page[i] = now.page[i] < 0 ? 0 : now.page[i];
+            now.page[i] = now.page[i] < a.pages ? now.page[i] : a.pages - 1;
         }
-        auto key_row = [&](int s) __attribute__((always_inline)) -> const char * {
-            if constexpr (BYPAGE) return kp[s] + mine * bytes;
-            const int32_t x = base + 16 * s + mine;
-            return token_at(a.k, a, w, x < keys.n ? x : keys.n - 1, sizeof(T));
+        const char *row16[kSub];
+        if constexpr (BYPAGE) {
+#pragma unroll
+            for (int s = 0; s < kSub; ++s)
+                row16[s] = keys_at + (uint64_t)(uint32_t)now.page[s] * a.page_bytes + (uint32_t)(((base + 16 * s) & slots) * bytes);
+        }
+        // (rows past the last key are of its page, or the last key's: theirs is taken by nobody)
+        auto row_of = [&](int s, int x) __attribute__((always_inline)) -> const char * {
+            if constexpr (BYPAGE) return row16[s] + x * bytes;
+            const int32_t page = __shfl(now.page[0], 16 * s + x, kWave), token = base + 16 * s + x;
+            return keys_at + (uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((token < keys.n ? token : keys.n - 1) & slots) * bytes);
         };
-        auto value_row = [&](int e) __attribute__((always_inline)) -> const char * {
-            if constexpr (BYPAGE) return vp[e >> 2] + (quarter * 4 + (e & 3)) * bytes;
-            const int32_t x = base + 16 * (e >> 2) + quarter * 4 + (e & 3);
-            return token_at(a.v, a, w, x < keys.n ? x : keys.n - 1, sizeof(T));
-        };
+        auto key_row = [&](int s) __attribute__((always_inline)) { return row_of(s, mine); };
+        auto value_row = [&](int e) __attribute__((always_inline)) { return row_of(e >> 2, quarter * 4 + (e & 3)) + values_behind; };
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
             const char *const row = key_row(s);
@@ -466,10 +491,33 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         }
     }
 
-    // the four waves' parts
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     if (l != l && m == kNone) m = 0.f;                 // (a query that is no number: its maximum says nothing, its sum does)
+    if constexpr (WAVES == 1) {
+        // a lane has kEach values after each other of its query
+        if (!w.valid) return;
+        const int64_t row = w.token * a.heads + w.qhead, at_part = row * a.parts + piece.part0 + part;
+        const float by = a.parts > 1 ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
+        if (a.parts > 1 && quarter == 0) a.stats[at_part] = float2{m, l};
+        if (a.parts > 1 && m == kNone) return;
+        T *const out = (T *)a.out + w.token * a.ldo + (int64_t)w.qhead * a.dim;
+        float *const sums_out = a.sums + at_part * a.dim;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int32_t d = (c * 16 + quarter * 4 + r) * kEach;
+                if (!FULL && d >= a.dim) continue;
+                float y[kEach];
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) y[e] = o[c][e][r] * by;
+                if (a.parts > 1) store_some(sums_out + d, y);
+                else store_some(out + d, y);
+            }
+        return;
+    }
+    // the four waves' parts
     if (quarter == 0) stats[wave][mine] = float2{m, l};
     if (threadIdx.x < 16) rows_at[mine] = w.valid ? w.token * a.heads + w.qhead : -1;
     __syncthreads();
@@ -985,8 +1033,13 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPi
     uint32_t b = blockIdx.x, item;
     int32_t part;
     const AttendPiece &piece = first_piece(p, &b) ? p.piece[0] : p.piece[1];
+    if (piece.alone) {
+        item = b * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item < piece.items) attend_rows<T, DP, FULL, BYPAGE, 1>(a, piece, item, 0, shared);
+        return;
+    }
     item_of(piece, b, &item, &part);
-    attend_rows<T, DP, FULL, BYPAGE>(a, piece, item, part, shared);
+    attend_rows<T, DP, FULL, BYPAGE, 4>(a, piece, item, part, shared);
 }
 
 template <int DP, bool FULL, bool BYPAGE>
@@ -1011,9 +1064,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_both_kernel(Att
     if (first_piece(p, &b)) {
         item_of(p.piece[0], b, &item, &part);
         attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared.tiles);
+    } else if (p.piece[1].alone) {
+        item = b * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item < p.piece[1].items) attend_rows<uint16_t, DP, FULL, BYPAGE, 1>(a, p.piece[1], item, 0, shared.rows);
     } else {
         item_of(p.piece[1], b, &item, &part);
-        attend_rows<uint16_t, DP, FULL, BYPAGE>(a, p.piece[1], item, part, shared.rows);
+        attend_rows<uint16_t, DP, FULL, BYPAGE, 4>(a, p.piece[1], item, part, shared.rows);
     }
 }
 
@@ -1116,7 +1172,10 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         *parts += x.parts;
         fits = fits && groups * tiles * x.parts <= 0x7fffffffLL;
         x.groups = (uint32_t)groups;
-        x.blocks = (uint32_t)(groups * tiles);
+        x.items = x.blocks = (uint32_t)(groups * tiles);
+        // many short rows: one a wave
+        x.alone = mode == kAttendOwn && x.parts == 1 && room <= 512 && groups * tiles >= 8 * (int64_t)ctx->num_cus;
+        if (x.alone) x.blocks = (x.items + 3) / 4;
     };
     // many queries that share a key head: by tiles of 128
     const bool bf16 = a.dtype == AS_BF16;

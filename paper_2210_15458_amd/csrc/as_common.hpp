@@ -393,7 +393,9 @@ struct AttendArgs {
 enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
 struct AttendPiece {             // one kind of work: which keys and queries
     int mode, queries;           // queries: of a block
-    uint32_t groups, blocks;     // blocks: of each part, `tiles` a group
+    uint32_t groups, items;      // `tiles` items a group
+    uint32_t blocks;             // of each part
+    bool alone;                  // an item a wave, four a block; otherwise one a block
     int32_t tiles;               // blocks after each other that read the same keys
     int32_t part0, parts;        // the parts that it leaves
     int32_t least;               // tiles of keys that a part takes at least
