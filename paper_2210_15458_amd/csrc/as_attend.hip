@@ -35,26 +35,33 @@ __device__ __forceinline__ int64_t offset_at(const AttendArgs &a, int64_t s)
     const int64_t o = a.offsets[s];
     return o < 0 ? 0 : o > a.tokens ? a.tokens : o;
 }
-// The last sequence whose first slot is at most `slot` (ROWS 0: whose first token is); 64 of them looked at at once.
-template <int ROWS> __device__ __forceinline__ int64_t find_sequence(const AttendArgs &a, int64_t slot, uint32_t group, uint32_t rows = ROWS)
+// The last sequence whose first slot is at most `slot` (ROWS 0: whose first token is), and its tokens; 64 of them looked at at once.
+struct Found {
+    int64_t s, from, to;
+};
+template <int ROWS> __device__ __forceinline__ Found find_sequence(const AttendArgs &a, int64_t slot, uint32_t group, uint32_t rows = ROWS)
 {
     int64_t lo = 0, hi = a.rows;                       // the answer is in [lo, hi)
-    while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) >> 6, s = lo + (lane_id() + 1) * step;
-        bool behind = false;
-        if (s < hi) {
-            const uint64_t o = offset_at(a, s);
-            behind = (int64_t)(ROWS > 0 ? o * group / rows + s : o) <= slot;
+    for (;;) {
+        const int64_t step = hi - lo > 63 ? (hi - lo + 62) / 63 : 1, s = lo + lane_id() * step;
+        const uint64_t o = s <= a.rows ? offset_at(a, s) : 0;
+        const bool behind = s < hi && (int64_t)(ROWS > 0 ? o * group / rows + s : o) <= slot;
+        int n = __popcll(__ballot(behind));            // (monotone: the first n lanes; the first of all in any case)
+        n = n > 0 ? n : 1;
+        lo += (n - 1) * step;
+        if (step == 1) {                               // (n is at most 63)
+            const uint32_t low = (uint32_t)o, high = (uint32_t)(o >> 32);
+            Found f;
+            f.s = lo;
+            f.from = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, n - 1) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, n - 1));
+            f.to = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, n) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, n));
+            return f;
         }
-        const int n = __popcll(__ballot(behind));      // (monotone: the first n lanes)
-        const int64_t next = lo + n * step;
-        hi = next + step < hi ? next + step : hi;
-        lo = next;
+        hi = lo + step < hi ? lo + step : hi;
     }
-    return lo;
 }
 
-// What a block works on: up to `rows` queries that share a key head, and a segment of keys.
+// What a block works on: up to ROWS queries that share a key head, and a segment of keys.
 struct Work {
     int32_t head;                 // key head
     const int32_t *table;         // the segment's pages
@@ -64,6 +71,8 @@ struct Work {
     bool valid;
     int64_t token;
     int32_t qhead, at;
+    // the smallest and largest position of the block's queries, and of those of the lane's wave (none: -1 as the largest)
+    int32_t lo, hi, wave_lo, wave_hi;
 };
 
 __device__ __forceinline__ int32_t length_of(const int32_t *lens, int64_t i, int32_t room)
@@ -72,10 +81,10 @@ __device__ __forceinline__ int32_t length_of(const int32_t *lens, int64_t i, int
     return n < 0 ? 0 : n > room ? room : n;
 }
 
-// Query `mine` of the ROWS of an item.  False where the block has nothing to do.  (The launch sees to it that a sequence's queries
-// times the heads of a group fit 32 bits.)
-template <int ROWS>
-__device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece &piece, uint32_t mine, uint32_t item, Work &w)
+// Query `mine` of the ROWS of an item, for a wave that has EACH of them from wave_from on.  False where the block has nothing to
+// do.  (The launch sees to it that a sequence's queries times the heads of a group fit 32 bits.)
+template <int ROWS, int EACH>
+__device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece &piece, uint32_t mine, uint32_t wave_from, uint32_t item, Work &w)
 {
     const uint32_t G = a.group;
     // x / G for x < G + 128
@@ -83,22 +92,28 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
     if (piece.mode == kAttendRagged) {
         const uint32_t slot = item / (uint32_t)a.kv_heads;
         w.head = (int32_t)(item - slot * a.kv_heads);
-        const int64_t s = find_sequence<ROWS>(a, slot, G);
-        const int64_t from = offset_at(a, s), to = offset_at(a, s + 1);
-        const int32_t len = length_of(a.lens, s, a.room);
-        const int64_t first = ((int64_t)slot - s - (int64_t)((uint64_t)from * G / ROWS)) * ROWS;      // the tile's first row in its sequence
-        const int64_t all = (to - from) * G;
+        const Found f = find_sequence<ROWS>(a, slot, G);
+        const int32_t len = length_of(a.lens, f.s, a.room);
+        const int64_t first = ((int64_t)slot - f.s - (int64_t)((uint64_t)f.from * G / ROWS)) * ROWS;      // the tile's first row in its sequence
+        const int64_t all = (f.to - f.from) * G;
         // (below 0: offsets that fall)
-        if (first < 0 || first >= all || (a.finished && a.finished[s])) return false;
-        w.table = a.table + s * a.table_ld;
+        if (first < 0 || first >= all || (a.finished && a.finished[f.s])) return false;
+        w.table = a.table + f.s * a.table_ld;
         w.n = len;
         w.key0 = 0;
-        const uint32_t first_token = (uint32_t)first / G, rest = (uint32_t)first - first_token * G, left = (uint32_t)(all - first);
+        const uint32_t first_token = (uint32_t)first / G, rest = (uint32_t)first - first_token * G;
+        const uint32_t left = all - first < ROWS ? (uint32_t)(all - first) : ROWS;
         w.valid = mine < left;
         const uint32_t x = rest + (w.valid ? mine : left - 1), i = by_group(x);
-        w.token = from + first_token + i;
+        const int32_t first_at = len - (int32_t)(f.to - f.from) + (int32_t)first_token;
+        w.token = f.from + first_token + i;
         w.qhead = (int32_t)(w.head * G + x - i * G);
-        w.at = len - (int32_t)(to - from) + (int32_t)(first_token + i);
+        w.at = first_at + (int32_t)i;
+        const uint32_t wave_to = wave_from + EACH < left ? wave_from + EACH : left;
+        w.lo = first_at;
+        w.hi = first_at + (int32_t)by_group(rest + left - 1);
+        w.wave_lo = first_at + (int32_t)by_group(rest + wave_from);
+        w.wave_hi = wave_from < left ? first_at + (int32_t)by_group(rest + wave_to - 1) : -1;
         return true;
     }
     const uint32_t group = item / (uint32_t)piece.tiles, tile = item - group * piece.tiles;
@@ -113,7 +128,7 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
         w.table = a.table + p * a.table_ld;
         w.n = length_of(a.lens, p, a.room);
         w.key0 = a.prompt_table ? length_of(a.prompt_lens, p / (uint32_t)a.per, a.prompt_room) : 0;
-        w.at = w.n - 1;
+        w.at = w.lo = w.hi = w.wave_lo = w.wave_hi = w.n - 1;
         return true;
     }
     w.table = a.prompt_table + p * a.prompt_table_ld;
@@ -125,12 +140,43 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
     if (w.valid && a.finished && a.finished[row]) w.valid = false;
     w.token = row;
     w.qhead = (int32_t)(w.head * G + x - c * G);
-    int32_t own = 0;
-    if (w.valid && a.table) {
-        own = a.lens[row];
-        own = own < 0 ? 0 : own > a.room ? a.room : own;
+    w.at = w.lo = w.hi = w.wave_lo = w.n - 1;
+    w.wave_hi = first + wave_from < (uint32_t)a.per * G ? w.n - 1 : -1;
+    if (a.window > 0) {
+        // rows are as far behind their prompt as they have tokens of their own (without a window they see all of it)
+        int32_t own = 0;
+        if (w.valid && a.table) {
+            own = a.lens[row];
+            own = own < 0 ? 0 : own > a.room ? a.room : own;
+        }
+        w.at += own;
+        int32_t lo = w.valid ? w.at : 0x7fffffff, hi = w.valid ? w.at : -1;
+#pragma unroll
+        for (int d = 1; d < EACH; d <<= 1) {
+            const int32_t u = __shfl_xor(lo, d, kWave), v = __shfl_xor(hi, d, kWave);
+            lo = u < lo ? u : lo;
+            hi = v > hi ? v : hi;
+        }
+        w.lo = w.wave_lo = __builtin_amdgcn_readfirstlane(lo);
+        w.hi = w.wave_hi = __builtin_amdgcn_readfirstlane(hi);
+        if (ROWS > EACH) {
+            __shared__ int32_t ends[2][4];
+            const int wave = threadIdx.x >> 6;
+            if (lane_id() == 0) {
+                ends[0][wave] = lo;
+                ends[1][wave] = hi;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w.lo = ends[0][i] < w.lo ? ends[0][i] : w.lo;
+                w.hi = ends[1][i] > w.hi ? ends[1][i] : w.hi;
+            }
+            w.lo = __builtin_amdgcn_readfirstlane(w.lo);
+            w.hi = __builtin_amdgcn_readfirstlane(w.hi);
+        }
+        if (w.lo > w.hi) w.lo = w.hi;                  // (no query)
     }
-    w.at = w.n + own - 1;
     return true;
 }
 
@@ -263,7 +309,8 @@ template <class T, int DP> struct RowsShared {
     static constexpr int kStride = DP + 4;
     __attribute__((aligned(16))) float sums[4 * 16 * kStride];
     float2 stats[4][16];
-    int64_t rows_at[16];                               // token * heads + head of each query, -1: none
+    int64_t token[16];                                 // of each query, -1: none ...
+    int32_t head[16];                                  // ... and its head
 };
 
 template <class T, int DP, bool FULL, bool BYPAGE, int WAVES>
@@ -275,22 +322,12 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     constexpr bool kBf16 = sizeof(T) == 2;
     float *const sums = shared.sums;
     float2(*const stats)[16] = shared.stats;
-    int64_t *const rows_at = shared.rows_at;
     const int lane = threadIdx.x & 63, quarter = lane >> 4, mine = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * (int32_t)sizeof(T);
     Work w;
-    if (!find_work<16>(a, piece, mine, item, w)) return;
-    int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = w.valid ? w.at : -1;
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        const int32_t u = __shfl_xor(lo_at, d, kWave), v = __shfl_xor(hi_at, d, kWave);
-        lo_at = u < lo_at ? u : lo_at;
-        hi_at = v > hi_at ? v : hi_at;
-    }
-    lo_at = __builtin_amdgcn_readfirstlane(lo_at);
-    hi_at = __builtin_amdgcn_readfirstlane(hi_at);
-    if (lo_at > hi_at) lo_at = hi_at;                  // (no query)
+    if (!find_work<16, 16>(a, piece, mine, 0, item, w)) return;
+    const int32_t lo_at = w.lo, hi_at = w.hi;
     const Keys keys = keys_of(a, w, lo_at, hi_at, BN, part, piece.parts, piece.least);
     const int32_t at = w.valid ? w.at : -1;
     const int32_t first = keys.first + (WAVES > 1 ? wave : 0), last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0;
@@ -519,7 +556,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     }
     // the four waves' parts
     if (quarter == 0) stats[wave][mine] = float2{m, l};
-    if (threadIdx.x < 16) rows_at[mine] = w.valid ? w.token * a.heads + w.qhead : -1;
+    if (threadIdx.x < 16) {
+        shared.token[mine] = w.valid ? w.token : -1;
+        shared.head[mine] = w.qhead;
+    }
     __syncthreads();
     float M = kNone;
 #pragma unroll
@@ -543,8 +583,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     for (int i = threadIdx.x; i < 16 * (DP / 8); i += 256) {
         const int r = i / (DP / 8), d = i % (DP / 8) * 8;
         if (d >= a.dim) continue;
-        const int64_t row = rows_at[r];
-        if (row < 0) continue;
+        const int64_t token = shared.token[r];
+        const int32_t head = shared.head[r];
+        if (token < 0) continue;
         float top = kNone, total = 0.f, y[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, stats[j][r].x);
@@ -561,10 +602,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             const float inverse = total > 0.f || total != total ? 1.f / total : 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= inverse;
-            const int64_t token = row / a.heads;
-            store8((T *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
+            store8((T *)a.out + token * a.ldo + (int64_t)head * a.dim + d, y);
         } else {
-            const int64_t at_part = row * a.parts + piece.part0 + part;
+            const int64_t at_part = (token * a.heads + head) * a.parts + piece.part0 + part;
             if (d == 0) a.stats[at_part] = float2{top, total};
             if (top != kNone) store8(a.sums + at_part * a.dim + d, y);
         }
@@ -631,8 +671,9 @@ __device__ __forceinline__ void tile_barrier()
 
 template <int DP> struct TilesShared {
     __attribute__((aligned(1024))) unsigned char smem[TileForm<DP>::kLds];
-    int64_t rows_at[TileForm<DP>::kQueries];
-    int32_t ends[2][4], any_odd;
+    int64_t token[TileForm<DP>::kQueries];             // of each query, -1: none ...
+    int32_t head[TileForm<DP>::kQueries];              // ... and its head
+    int32_t any_odd;
 };
 
 // The other half of a wave's value beside a lane's own.
@@ -648,32 +689,22 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     typedef TileForm<DP> F;
     constexpr int BN = F::kKeys, kLoads = F::kLoads, kPieces = F::kPieces, kStride = F::kStride, kRow = DP * 2;
     unsigned char *const smem = shared.smem;
-    int64_t *const rows_at = shared.rows_at;
-    int32_t(*const ends)[4] = shared.ends;
     int32_t &any_odd = shared.any_odd;
     const int lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * 2;
     Work w;
-    if (!find_work<F::kQueries>(a, piece, wave * 32 + mine, item, w)) return;
+    if (!find_work<F::kQueries, 32>(a, piece, wave * 32 + mine, wave * 32, item, w)) return;
     const int32_t at = w.valid ? w.at : -1;
-    int32_t lo_at = w.valid ? w.at : 0x7fffffff, hi_at = at;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t u = __shfl_xor(lo_at, d, kWave), v = __shfl_xor(hi_at, d, kWave);
-        lo_at = u < lo_at ? u : lo_at;
-        hi_at = v > hi_at ? v : hi_at;
-    }
-    if (lane < 32) rows_at[wave * 32 + mine] = w.valid ? w.token * a.heads + w.qhead : -1;
-    if (lane == 0) {
-        ends[0][wave] = lo_at;
-        ends[1][wave] = hi_at;
+    if (lane < 32) {
+        shared.token[wave * 32 + mine] = w.valid ? w.token : -1;
+        shared.head[wave * 32 + mine] = w.qhead;
     }
     if (threadIdx.x == 0) any_odd = 0;
     if (!FULL) {                                       // what lies past the rows' ends is never written to again
         for (int i = threadIdx.x; i < 4 * F::kBytes / 16; i += 256) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
     }
-    const int32_t wave_lo = __builtin_amdgcn_readfirstlane(lo_at), wave_hi = __builtin_amdgcn_readfirstlane(hi_at);
+    const int32_t lo = w.lo, hi = w.hi, wave_lo = w.wave_lo, wave_hi = w.wave_hi;
     // the queries (zeros where there is none and past the row's end)
     u32x4 q[DP / 16];
     {
@@ -688,16 +719,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         }
     }
     const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
-    __syncthreads();
-    int32_t lo = ends[0][0], hi = ends[1][0];
-#pragma unroll
-    for (int i = 1; i < 4; ++i) {
-        lo = ends[0][i] < lo ? ends[0][i] : lo;
-        hi = ends[1][i] > hi ? ends[1][i] : hi;
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    hi = __builtin_amdgcn_readfirstlane(hi);
-    if (lo > hi) lo = hi;
+    if (!FULL) __syncthreads();
     const Keys keys = keys_of(a, w, lo, hi, BN, part, piece.parts, piece.least);
 
     // What a wave fetches of a tile: BN / 4 rows after each other (all in one page, of pages of 16 tokens and more), kLoads KiB, of which
@@ -961,18 +983,18 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = i * 8 + lane / 8, d = c * 64 + lane % 8 * 8;
-            const int64_t row = rows_at[wave * 32 + r];
+            const int64_t token = shared.token[wave * 32 + r];
+            const int32_t head = shared.head[wave * 32 + r];
             const float ml = __shfl(m, r, kWave), ll = __shfl(l, r, kWave);
-            if (row < 0 || d >= a.dim) continue;
+            if (token < 0 || d >= a.dim) continue;
             float y[8];
             const float *const from = sums + r * kStride + lane % 8 * 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = from[e];
             if (a.parts == 1) {
-                const int64_t token = row / a.heads;
-                store8((uint16_t *)a.out + token * a.ldo + (row - token * a.heads) * a.dim + d, y);
+                store8((uint16_t *)a.out + token * a.ldo + (int64_t)head * a.dim + d, y);
             } else {
-                const int64_t at_part = row * a.parts + piece.part0 + part;
+                const int64_t at_part = (token * a.heads + head) * a.parts + piece.part0 + part;
                 if (d == 0) a.stats[at_part] = float2{ml, ll};
                 if (ml != kNone) store8(a.sums + at_part * a.dim + d, y);
             }
@@ -1080,22 +1102,22 @@ template <class T>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t token = i / a.heads;
+    const uint32_t i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t token = i / (uint32_t)a.heads;       // (the launch sees to it that they fit)
     if (token >= a.tokens) return;
     if (a.offsets) {
         if (token < offset_at(a, 0) || token >= offset_at(a, a.rows)) return;
-        if (a.finished && a.finished[find_sequence<0>(a, token, 1)]) return;
+        if (a.finished && a.finished[find_sequence<0>(a, token, 1).s]) return;
     } else if (a.finished && a.finished[token]) return;
-    const float2 *const stats = a.stats + i * a.parts;
+    const float2 *const stats = a.stats + (int64_t)i * a.parts;
     const float2 mine = lane < a.parts ? stats[lane] : float2{kNone, 0.f};
     const float M = wave_max(mine.x);
     const float weight = mine.x == kNone ? 0.f : __builtin_amdgcn_exp2f(mine.x - M);
     const float total = wave_sum(weight * mine.y);
     const float inverse = total > 0.f || total != total ? 1.f / total : 0.f;
     const uint64_t there = __ballot(mine.x != kNone);
-    const float *const sums = a.sums + i * a.parts * a.dim;
-    T *const out = (T *)a.out + token * a.ldo + (i - token * a.heads) * a.dim;
+    const float *const sums = a.sums + (int64_t)i * a.parts * a.dim;
+    T *const out = (T *)a.out + token * a.ldo + ((int64_t)i - token * a.heads) * a.dim;
     for (int32_t d = lane * 8; d < a.dim; d += kWave * 8) {
         float y[8];
 #pragma unroll
@@ -1196,7 +1218,8 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         p.every = (uint32_t)(1 + second / (2 * first));
         fits = fits && first + second <= 0x7fffffffLL;
     }
-    *fit = fits;
+    // (and the queries' heads, where they are joined)
+    *fit = fits && (*parts < 2 || a.tokens * a.heads <= 0x7fffffffLL);
     return p;
 }
 
@@ -1241,9 +1264,10 @@ __global__ __launch_bounds__(256) void cache_add_kernel(AttendArgs a, const void
     const int32_t per_head = a.dim * esz / 16, pieces = 2 * a.kv_heads * per_head;
     int64_t s = 0, from = 0, to = 0, first;
     if (a.offsets) {
-        s = find_sequence<1>(a, blockIdx.x, 1, tokens_each);
-        from = offset_at(a, s);
-        to = offset_at(a, s + 1);
+        const Found f = find_sequence<1>(a, blockIdx.x, 1, tokens_each);
+        s = f.s;
+        from = f.from;
+        to = f.to;
         first = from + ((int64_t)blockIdx.x - s - from / tokens_each) * tokens_each;
         if (first < from || first >= to || (a.finished && a.finished[s])) return;
     } else {
