@@ -500,7 +500,7 @@ class Cache:
         page = self.kv_heads * self.page_size * self.head_dim
         if pages and (not k[0].is_contiguous() or (pages > 1 and k.stride(0) < page)):
             raise ValueError("the pages of k and v must be contiguous, one behind the other")
-        self.torch_dtype, self.device = k.dtype, k.device
+        self.torch_dtype, self.index, self.scale = k.dtype, k.get_device(), self.head_dim ** -0.5
         self._tensors = (k, v)
         c = self._c = _Cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else page, self.page_size, self.kv_heads, self.head_dim,
                              _dtype_code(k))
@@ -513,10 +513,10 @@ class Sequences:
     def __init__(self, rows, table=None, lens=None, prompt_table=None, prompt_lens=None, rows_per_prompt=1, finished=None):
         self.rows = int(rows)
         self._tensors = (table, lens, prompt_table, prompt_lens, finished)
-        devices = {t.device for t in self._tensors if t is not None}
+        devices = {t.get_device() for t in self._tensors if t is not None}
         if len(devices) > 1:
             raise ValueError("the sequences' tensors must be on one device")
-        self.device = devices.pop() if devices else None
+        self.index = devices.pop() if devices else None
         c = self._c = _Sequences()
         if (table is None) != (lens is None) or (prompt_table is None) != (prompt_lens is None):
             raise ValueError("a table needs its lengths, and lengths a table")
@@ -541,55 +541,75 @@ class Sequences:
         return ptr, ld
 
 
-def _tokens_of(ctx, cache, seqs, t, dtype, name, rows, cols):
-    if isinstance(t, torch.Tensor) and t.dim() == 3 and t.stride(2) == 1 and (t.size(1) < 2 or t.stride(1) == t.size(2)):
-        t = t.as_strided((t.size(0), t.size(1) * t.size(2)), (t.stride(0), 1))
-    got = _rows(t, dtype, name, rows, cols)
-    if t.device != cache.device or (seqs.device is not None and seqs.device != cache.device) or ctx.stream.device != cache.device:
-        raise ValueError(f"{name}, the cache, the sequences and the context must be on one device")
-    return got
+def _one_device(ctx, cache, seqs):
+    if seqs.index not in (None, cache.index) or ctx.stream.device_index != cache.index:
+        raise ValueError("the cache, the sequences and the context must be on one device")
+
+
+def _tokens_of(cache, t, name, rows, cols):
+    """Pointer and row stride of rows of heads, [tokens, heads * head_dim] or [tokens, heads, head_dim], on the cache's device."""
+    if isinstance(t, torch.Tensor):
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 3 and shape[1] * shape[2] == cols and stride[2] == 1 and (shape[1] < 2 or stride[1] == shape[2]):
+            shape, stride = (shape[0], cols), (stride[0], 1)
+        if (len(shape) == 2 and t.dtype is cache.torch_dtype and t.get_device() == cache.index and shape[0] >= rows and shape[1] >= cols
+                and stride[1] == 1 and (stride[0] >= shape[1] or shape[0] < 2)):
+            return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
+        if t.is_cuda and t.get_device() != cache.index:
+            raise ValueError(f"{name} must be on the cache's device")
+        if t.dim() == 3:
+            raise ValueError(f"{name} must be [tokens, heads, head_dim] with a token's heads one behind the other, {rows} tokens of {cols} values")
+    return _rows(t, cache.torch_dtype, name, rows, cols)        # (which says what it is)
 
 
 def _offsets_of(cache, seqs, offsets):
-    if offsets.device != cache.device:
+    ptr = _dev(offsets, torch.int64, "offsets", seqs.rows + 1)
+    if offsets.get_device() != cache.index:
         raise ValueError("offsets must be on the cache's device")
-    return _dev(offsets, torch.int64, "offsets", seqs.rows + 1)
+    return ptr
 
 
 def as_cache_add(ctx, cache, seqs, k, v, offsets=None):
     """Keys and values [tokens, kv_heads * head_dim] (or [tokens, kv_heads, head_dim]) of the rows' last tokens into their pages:
     one a row, or with offsets [rows + 1] as many as they say."""
-    n, dtype, cols = k.size(0), cache.torch_dtype, cache.kv_heads * cache.head_dim
-    if offsets is None and n < seqs.rows:
-        raise ValueError(f"k has {n} rows, needs {seqs.rows}")
-    n = seqs.rows if offsets is None else n
-    kp, ldk = _tokens_of(ctx, cache, seqs, k, dtype, "k", n, cols)
-    vp, ldv = _tokens_of(ctx, cache, seqs, v, dtype, "v", n, cols)
-    ctx._check(lib().as_cache_add(ctx._h, cache._ref, seqs._ref, seqs.rows, kp, ldk, vp, ldv, n, None if offsets is None else _offsets_of(cache, seqs, offsets)))
+    _one_device(ctx, cache, seqs)
+    cols = cache.kv_heads * cache.head_dim
+    n, at = (seqs.rows, None) if offsets is None else (k.size(0), _offsets_of(cache, seqs, offsets))
+    kp, ldk = _tokens_of(cache, k, "k", n, cols)
+    vp, ldv = _tokens_of(cache, v, "v", n, cols)
+    rc = (_lib or lib()).as_cache_add(ctx._h, cache._ref, seqs._ref, seqs.rows, kp, ldk, vp, ldv, n, at)
+    if rc:
+        ctx._check(rc)
 
 
 def _heads_of(cache, q):
-    cols = q.size(1) if q.dim() == 2 else q.size(1) * q.size(2)
-    if cols % cache.head_dim:
+    cols = q.shape[1] if len(q.shape) == 2 else q.shape[1] * q.shape[2]
+    heads = cols // cache.head_dim
+    if heads * cache.head_dim != cols:
         raise ValueError(f"q has {cols} columns, no whole number of heads of {cache.head_dim}")
-    return cols // cache.head_dim
+    return heads, cols
 
 
 def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
     """Attention of one query a row, q and out [rows, heads * head_dim] (or [rows, heads, head_dim]); scale: 1 / sqrt(head_dim)."""
-    heads, rows = _heads_of(cache, q), seqs.rows
-    qp, ldq = _tokens_of(ctx, cache, seqs, q, cache.torch_dtype, "q", rows, heads * cache.head_dim)
-    op, ldo = _tokens_of(ctx, cache, seqs, out, cache.torch_dtype, "out", rows, heads * cache.head_dim)
-    rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.head_dim ** -0.5 if scale is None else float(scale),
-                                   int(window), int(sinks), op, ldo)
+    _one_device(ctx, cache, seqs)
+    heads, cols = _heads_of(cache, q)
+    rows = seqs.rows
+    qp, ldq = _tokens_of(cache, q, "q", rows, cols)
+    op, ldo = _tokens_of(cache, out, "out", rows, cols)
+    rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.scale if scale is None else scale, window, sinks, op, ldo)
     if rc:
         ctx._check(rc)
 
 
 def as_attend_prompts(ctx, cache, seqs, q, offsets, out, scale=None, window=0, sinks=0):
     """The same for ragged queries: row r has q[offsets[r]:offsets[r + 1]], those of its last tokens."""
-    heads, n = _heads_of(cache, q), q.size(0)
-    qp, ldq = _tokens_of(ctx, cache, seqs, q, cache.torch_dtype, "q", n, heads * cache.head_dim)
-    op, ldo = _tokens_of(ctx, cache, seqs, out, cache.torch_dtype, "out", n, heads * cache.head_dim)
-    ctx._check(lib().as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, _offsets_of(cache, seqs, offsets), heads,
-                                       cache.head_dim ** -0.5 if scale is None else float(scale), int(window), int(sinks), op, ldo))
+    _one_device(ctx, cache, seqs)
+    heads, cols = _heads_of(cache, q)
+    n, at = q.size(0), _offsets_of(cache, seqs, offsets)
+    qp, ldq = _tokens_of(cache, q, "q", n, cols)
+    op, ldo = _tokens_of(cache, out, "out", n, cols)
+    rc = (_lib or lib()).as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, at, heads, cache.scale if scale is None else scale,
+                                           window, sinks, op, ldo)
+    if rc:
+        ctx._check(rc)

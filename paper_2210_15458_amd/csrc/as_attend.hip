@@ -1168,10 +1168,12 @@ static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &
     else launch_pieces<T, 256>(ctx, a, p, grid);
 }
 
-// Parts that the keys of each query are split into: two blocks a compute unit, if each still has so many keys.
-static int32_t parts_for(const as_ctx *ctx, int64_t blocks, int64_t room, int64_t least)
+// Parts that the keys of each query are split into: two blocks a compute unit, if each still has `least` keys.  Joining costs all
+// queries a pass over their parts, and prompts have many: they are split only where half of the units would have no block
+// (8192 tokens in 416 blocks: 16 us whole, 37 in two parts; 1024 rows over shared prompts of 512 21 whole, 18 in two, 23 in four).
+static int32_t parts_for(const as_ctx *ctx, int mode, int64_t blocks, int64_t room, int64_t least)
 {
-    int64_t n = (2 * (int64_t)ctx->num_cus + blocks - 1) / blocks;
+    int64_t n = mode == kAttendRagged ? ctx->num_cus / blocks : (2 * (int64_t)ctx->num_cus + blocks - 1) / blocks;
     const int64_t most = (room + least - 1) / least;
     n = n < most ? n : most;
     return (int32_t)(n < 1 ? 1 : n > kAttendMostParts ? kAttendMostParts : n);
@@ -1190,7 +1192,7 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         x.tiles = tiles;
         x.least = queries == 16 ? 8 : 4;
         x.part0 = *parts;
-        x.parts = parts_for(ctx, groups * tiles, room, queries == 16 ? 256 : 512);
+        x.parts = parts_for(ctx, mode, groups * tiles, room, 256);
         *parts += x.parts;
         fits = fits && groups * tiles * x.parts <= 0x7fffffffLL;
         x.groups = (uint32_t)groups;
