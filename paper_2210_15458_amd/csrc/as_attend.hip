@@ -83,13 +83,13 @@ __device__ __forceinline__ int32_t length_of(const int32_t *lens, int64_t i, int
 
 // Query `mine` of the ROWS of an item, for a wave that has EACH of them from wave_from on.  False where the block has nothing to
 // do.  (The launch sees to it that a sequence's queries times the heads of a group fit 32 bits.)
-template <int ROWS, int EACH>
+template <int ROWS, int EACH, int MODE>
 __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece &piece, uint32_t mine, uint32_t wave_from, uint32_t item, Work &w)
 {
     const uint32_t G = a.group;
     // x / G for x < G + 128
     auto by_group = [&](uint32_t x) __attribute__((always_inline)) { return x * a.group_inverse >> 24; };
-    if (piece.mode == kAttendRagged) {
+    if constexpr (MODE == kAttendRagged) {
         const uint32_t slot = item / (uint32_t)a.kv_heads;
         w.head = (int32_t)(item - slot * a.kv_heads);
         const Found f = find_sequence<ROWS>(a, slot, G);
@@ -116,10 +116,10 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
         w.wave_hi = wave_from < left ? first_at + (int32_t)by_group(rest + wave_to - 1) : -1;
         return true;
     }
-    const uint32_t group = item / (uint32_t)piece.tiles, tile = item - group * piece.tiles;
+    const uint32_t group = MODE == kAttendOwn && piece.tiles == 1 ? item : item / (uint32_t)piece.tiles, tile = item - group * piece.tiles;
     const uint32_t p = group / (uint32_t)a.kv_heads;    // row or prompt
     w.head = (int32_t)(group - p * a.kv_heads);
-    if (piece.mode == kAttendOwn) {
+    if constexpr (MODE == kAttendOwn) {
         if (a.finished && a.finished[p]) return false;
         const uint32_t g = tile * ROWS + mine;
         w.valid = g < G;
@@ -313,7 +313,7 @@ template <class T, int DP> struct RowsShared {
     int32_t head[16];                                  // ... and its head
 };
 
-template <class T, int DP, bool FULL, bool BYPAGE, int WAVES>
+template <class T, int DP, bool FULL, bool BYPAGE, int WAVES, int MODE>
 __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, RowsShared<T, DP> &shared)
 {
     typedef AttendForm<T, DP> F;
@@ -326,7 +326,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * (int32_t)sizeof(T);
     Work w;
-    if (!find_work<16, 16>(a, piece, mine, 0, item, w)) return;
+    if (!find_work<16, 16, MODE>(a, piece, mine, 0, item, w)) return;
     const int32_t lo_at = w.lo, hi_at = w.hi;
     const Keys keys = keys_of(a, w, lo_at, hi_at, BN, part, piece.parts, piece.least);
     const int32_t at = w.valid ? w.at : -1;
@@ -468,7 +468,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             }
             // A value that is no number, seen by some queries and not by others of the tile: it is left out of the product, and
             // added to those that see it at the end.
-            if (lo_at != hi_at && __any(no_number<T>(largest))) {
+            if (MODE != kAttendOwn && lo_at != hi_at && __any(no_number<T>(largest))) {
                 odd = true;
 #pragma unroll
                 for (int e = 0; e < kSub * 4; ++e)
@@ -578,7 +578,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
                 *reinterpret_cast<f32x4 *>(to + e) = x;
             }
         }
-    if (odd) add_odd_values<T, 16>(a, w, keys, BN, wave, 4, at, sums + wave * 16 * kStride, kStride, 0, a.dim);
+    if (MODE != kAttendOwn && odd) add_odd_values<T, 16>(a, w, keys, BN, wave, 4, at, sums + wave * 16 * kStride, kStride, 0, a.dim);
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * (DP / 8); i += 256) {
         const int r = i / (DP / 8), d = i % (DP / 8) * 8;
@@ -683,7 +683,7 @@ __device__ __forceinline__ float halves_max(float x)
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-template <int DP, bool FULL, bool BYPAGE>
+template <int DP, bool FULL, bool BYPAGE, int MODE>
 __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPiece &piece, uint32_t item, int32_t part, TilesShared<DP> &shared)
 {
     typedef TileForm<DP> F;
@@ -694,7 +694,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t bytes = a.dim * 2;
     Work w;
-    if (!find_work<F::kQueries, 32>(a, piece, wave * 32 + mine, wave * 32, item, w)) return;
+    if (!find_work<F::kQueries, 32, MODE>(a, piece, wave * 32 + mine, wave * 32, item, w)) return;
     const int32_t at = w.valid ? w.at : -1;
     if (lane < 32) {
         shared.token[wave * 32 + mine] = w.valid ? w.token : -1;
@@ -1007,14 +1007,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 
 // Which work is block b's: of a piece's items, of which `tiles` after each other read the same keys, those of a group go to one
 // XCD (blocks go round the eight), whose L2 then has the keys; of ragged queries the last first, which see most keys.
-__device__ __forceinline__ void item_of(const AttendPiece &p, uint32_t b, uint32_t *item, int32_t *part)
+template <int MODE> __device__ __forceinline__ void item_of(const AttendPiece &p, uint32_t b, uint32_t *item, int32_t *part)
 {
     if (p.parts == 1 && p.tiles == 1) {
         *part = 0;
-        *item = p.mode == kAttendRagged ? p.blocks - 1 - b : b;
+        *item = MODE == kAttendRagged ? p.blocks - 1 - b : b;
         return;
     }
-    if (p.mode == kAttendRagged) {
+    if constexpr (MODE == kAttendRagged) {
         const uint32_t x = b / p.blocks;
         *part = (int32_t)x;
         *item = p.blocks - 1 - (b - x * p.blocks);
@@ -1048,34 +1048,45 @@ __device__ __forceinline__ bool first_piece(const AttendPieces &p, uint32_t *b)
     return false;
 }
 
+// A block's share of rows' own tokens.
 template <class T, int DP, bool FULL, bool BYPAGE>
+__device__ __forceinline__ void attend_own(const AttendArgs &a, const AttendPiece &piece, uint32_t b, RowsShared<T, DP> &shared)
+{
+    uint32_t item;
+    int32_t part;
+    if (piece.alone) {
+        item = b * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item < piece.items) attend_rows<T, DP, FULL, BYPAGE, 1, kAttendOwn>(a, piece, item, 0, shared);
+        return;
+    }
+    item_of<kAttendOwn>(piece, b, &item, &part);
+    attend_rows<T, DP, FULL, BYPAGE, 4, kAttendOwn>(a, piece, item, part, shared);
+}
+
+template <class T, int DP, bool FULL, bool BYPAGE>
+__global__ __launch_bounds__(256) void attend_own_kernel(AttendArgs a, AttendPieces p)
+{
+    __shared__ RowsShared<T, DP> shared;
+    attend_own<T, DP, FULL, BYPAGE>(a, p.piece[0], blockIdx.x, shared);
+}
+
+// Queries of prompts, or of rows that share a prompt (MODE) with what is the rows' own beside them: 16 a block, or 128.
+template <class T, int DP, bool FULL, bool BYPAGE, int MODE>
 __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ RowsShared<T, DP> shared;
     uint32_t b = blockIdx.x, item;
     int32_t part;
-    const AttendPiece &piece = first_piece(p, &b) ? p.piece[0] : p.piece[1];
-    if (piece.alone) {
-        item = b * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (item < piece.items) attend_rows<T, DP, FULL, BYPAGE, 1>(a, piece, item, 0, shared);
-        return;
+    if (MODE == kAttendRagged || first_piece(p, &b)) {
+        item_of<MODE>(p.piece[0], b, &item, &part);
+        attend_rows<T, DP, FULL, BYPAGE, 4, MODE>(a, p.piece[0], item, part, shared);
+    } else if constexpr (MODE != kAttendRagged) {
+        attend_own<T, DP, FULL, BYPAGE>(a, p.piece[1], b, shared);
     }
-    item_of(piece, b, &item, &part);
-    attend_rows<T, DP, FULL, BYPAGE, 4>(a, piece, item, part, shared);
 }
 
-template <int DP, bool FULL, bool BYPAGE>
+template <int DP, bool FULL, bool BYPAGE, int MODE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a, AttendPieces p)
-{
-    __shared__ TilesShared<DP> shared;
-    uint32_t item;
-    int32_t part;
-    item_of(p.piece[0], blockIdx.x, &item, &part);
-    attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared);
-}
-
-template <int DP, bool FULL, bool BYPAGE>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_both_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ union Shared {
         TilesShared<DP> tiles;
@@ -1083,15 +1094,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attend_both_kernel(Att
     } shared;
     uint32_t b = blockIdx.x, item;
     int32_t part;
-    if (first_piece(p, &b)) {
-        item_of(p.piece[0], b, &item, &part);
-        attend_tiles<DP, FULL, BYPAGE>(a, p.piece[0], item, part, shared.tiles);
-    } else if (p.piece[1].alone) {
-        item = b * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (item < p.piece[1].items) attend_rows<uint16_t, DP, FULL, BYPAGE, 1>(a, p.piece[1], item, 0, shared.rows);
-    } else {
-        item_of(p.piece[1], b, &item, &part);
-        attend_rows<uint16_t, DP, FULL, BYPAGE, 4>(a, p.piece[1], item, part, shared.rows);
+    if (MODE == kAttendRagged || first_piece(p, &b)) {
+        item_of<MODE>(p.piece[0], b, &item, &part);
+        attend_tiles<DP, FULL, BYPAGE, MODE>(a, p.piece[0], item, part, shared.tiles);
+    } else if constexpr (MODE != kAttendRagged) {
+        attend_own<uint16_t, DP, FULL, BYPAGE>(a, p.piece[1], b, shared.rows);
     }
 }
 
@@ -1141,17 +1148,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 template <class T, int DP, bool FULL, bool BYPAGE>
 static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
 {
+    const bool ragged = p.piece[0].mode == kAttendRagged;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, ctx->stream, a, p); };
+    if (p.piece[0].mode == kAttendOwn) return launch(attend_own_kernel<T, DP, FULL, BYPAGE>);
     if constexpr (sizeof(T) == 2) {
-        if (p.piece[0].queries == 128 && p.count == 2) {
-            hipLaunchKernelGGL((attend_both_kernel<DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
-            return;
-        }
         if (p.piece[0].queries == 128) {
-            hipLaunchKernelGGL((attend_tiles_kernel<DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
-            return;
+            if (ragged) return launch(attend_tiles_kernel<DP, FULL, BYPAGE, kAttendRagged>);
+            return launch(attend_tiles_kernel<DP, FULL, BYPAGE, kAttendShared>);
         }
     }
-    hipLaunchKernelGGL((attend_rows_kernel<T, DP, FULL, BYPAGE>), grid, dim3(256), 0, ctx->stream, a, p);
+    if (ragged) return launch(attend_rows_kernel<T, DP, FULL, BYPAGE, kAttendRagged>);
+    launch(attend_rows_kernel<T, DP, FULL, BYPAGE, kAttendShared>);
 }
 template <class T, int DP>
 static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
