@@ -344,6 +344,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         }
         return p;
     };
+    // (behind the wave's last tile that one again: what is loaded in advance is then of no use, but there)
+    auto tile_base = [&](int32_t t) __attribute__((always_inline)) { return keys.base(t < keys.last ? t : keys.last - 1 - (keys.last - 1 - first) % WAVES, BN); };
     Pages ahead;
     if (first < keys.last) ahead = find_pages(keys.base(first, BN));
 
@@ -369,48 +371,46 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     const int32_t slots = (1 << a.page_shift) - 1;
     const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
     const int64_t values_behind = (const char *)a.v - (const char *)a.k;
-#pragma unroll 1
-    for (int32_t t = first; t < keys.last; t += WAVES) {
-        const int32_t base = keys.base(t, BN);
-        u32x4 k[kSub][kKey];
-        uint32_t v[kSub * 4][kChunks][kWords];
-        Pages now = ahead;
-        if (t + WAVES < keys.last) ahead = find_pages(keys.base(t + WAVES, BN));
+    u32x4 k[kSub][kKey];
+    uint32_t v[kSub * 4][kChunks][kWords];
+    // where the rows of a tile's tokens are
+    struct Rows {
+        const char *row16[BYPAGE ? kSub : 1];
+        int32_t base, page;
+    };
+    auto rows_at = [&](int32_t base, Pages now) __attribute__((always_inline)) {
+        Rows at;
+        at.base = base;
 #pragma unroll
         for (int i = 0; i < (BYPAGE ? kSub : 1); ++i) {
             now.page[i] = now.page[i] < 0 ? 0 : now.page[i];
             now.page[i] = now.page[i] < a.pages ? now.page[i] : a.pages - 1;
+            at.row16[i] = keys_at + (uint64_t)(uint32_t)now.page[i] * a.page_bytes + (uint32_t)(((base + 16 * i) & slots) * bytes);
         }
-        const char *row16[kSub];
-        if constexpr (BYPAGE) {
-#pragma unroll
-            for (int s = 0; s < kSub; ++s)
-                row16[s] = keys_at + (uint64_t)(uint32_t)now.page[s] * a.page_bytes + (uint32_t)(((base + 16 * s) & slots) * bytes);
-        }
-        // (rows past the last key are of its page, or the last key's: theirs is taken by nobody)
-        auto row_of = [&](int s, int x) __attribute__((always_inline)) -> const char * {
-            if constexpr (BYPAGE) return row16[s] + x * bytes;
-            const int32_t page = __shfl(now.page[0], 16 * s + x, kWave), token = base + 16 * s + x;
-            return keys_at + (uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((token < keys.n ? token : keys.n - 1) & slots) * bytes);
-        };
-        auto key_row = [&](int s) __attribute__((always_inline)) { return row_of(s, mine); };
-        auto value_row = [&](int e) __attribute__((always_inline)) { return row_of(e >> 2, quarter * 4 + (e & 3)) + values_behind; };
+        at.page = now.page[0];
+        return at;
+    };
+    // (rows past the last key are of its page, or the last key's: theirs is taken by nobody)
+    auto row_of = [&](const Rows &at, int s, int x) __attribute__((always_inline)) -> const char * {
+        if constexpr (BYPAGE) return at.row16[s] + x * bytes;
+        const int32_t page = __shfl(at.page, 16 * s + x, kWave), token = at.base + 16 * s + x;
+        return keys_at + (uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((token < keys.n ? token : keys.n - 1) & slots) * bytes);
+    };
+    auto load_keys = [&](const Rows &at) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
-            const char *const row = key_row(s);
+            const char *const row = row_of(at, s, mine);
 #pragma unroll
             for (int i = 0; i < kKey; ++i) {
                 const int32_t at_byte = (i * 4 + quarter) * 16;
-                if (FULL) k[s][i] = *reinterpret_cast<const u32x4 *>(row + at_byte);
-                else {
-                    k[s][i] = *reinterpret_cast<const u32x4 *>(row + (at_byte < bytes ? at_byte : 0));
-                    if (at_byte >= bytes) k[s][i] = u32x4{0, 0, 0, 0};
-                }
+                k[s][i] = *reinterpret_cast<const u32x4 *>(row + (FULL || at_byte < bytes ? at_byte : 0));
             }
         }
+    };
+    auto load_values = [&](const Rows &at) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < kSub * 4; ++e) {
-            const char *const row = value_row(e);
+            const char *const row = row_of(at, e >> 2, quarter * 4 + (e & 3)) + values_behind;
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
                 const int32_t at_byte = (c * 16 + mine) * kVBytes;
@@ -424,12 +424,36 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[e][c][i] = x[i];
                 }
-                if (!FULL && at_byte >= bytes) {
-#pragma unroll
-                    for (int i = 0; i < kWords; ++i) v[e][c][i] = 0;
-                }
             }
         }
+    };
+    // what lies past the rows' ends
+    auto cut_keys = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kKey; ++i)
+#pragma unroll
+            for (int s = 0; s < kSub; ++s)
+                if (!FULL && (i * 4 + quarter) * 16 >= bytes) k[s][i] = u32x4{0, 0, 0, 0};
+    };
+    auto cut_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int e = 0; e < kSub * 4; ++e)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i)
+                    if (!FULL && (c * 16 + mine) * kVBytes >= bytes) v[e][c][i] = 0;
+    };
+    if (first < keys.last) {
+        const Rows at = rows_at(keys.base(first, BN), ahead);
+        ahead = find_pages(tile_base(first + WAVES));
+        load_keys(at);
+        load_values(at);
+    }
+#pragma unroll 1
+    for (int32_t t = first; t < keys.last; t += WAVES) {
+        const int32_t base = keys.base(t, BN);
+        cut_keys();
         // scores
         f32x4 s4[kSub];
 #pragma unroll
@@ -447,6 +471,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
                 }
             }
         }
+        // the next tile's keys take their registers, and its values theirs behind this tile's
+        const Rows next = rows_at(tile_base(t + WAVES), ahead);
+        ahead = find_pages(tile_base(t + 2 * WAVES));
+        load_keys(next);
+        cut_values();
         float p[kSub * 4];
 #pragma unroll
         for (int e = 0; e < kSub * 4; ++e) p[e] = s4[e >> 2][e & 3] * a.scale;
@@ -526,6 +555,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
                         o[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[j][c][e]), p[j], o[c][e], 0, 0, 0);
             }
         }
+        load_values(next);
     }
 
     l += __shfl_xor(l, 16, kWave);
