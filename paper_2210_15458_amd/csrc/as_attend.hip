@@ -293,10 +293,15 @@ template <int DP> struct AttendForm<uint16_t, DP> {
     static constexpr int kSub = 2, kKey = DP / 32, kVBytes = DP == 64 ? 8 : 16, kChunks = DP == 256 ? 2 : 1, kEach = kVBytes / 2;
 };
 template <int DP> struct AttendForm<float, DP> {
-    static constexpr int kSub = 1, kKey = DP / 16, kVBytes = 16, kChunks = DP / 64, kEach = 4;
+    static constexpr int kSub = 1, kKey = DP / 16, kVBytes = DP == 96 ? 8 : 16, kEach = kVBytes / 4, kChunks = DP / (16 * kEach);
 };
 
-// Four or eight values after each other.
+// Two, four or eight values after each other.
+__device__ __forceinline__ void store_some(float *p, const float (&y)[2])
+{
+    typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+    *reinterpret_cast<f32x2_any *>(p) = f32x2{y[0], y[1]};
+}
 __device__ __forceinline__ void store_some(float *p, const float (&y)[4]) { *reinterpret_cast<f32x4_any *>(p) = f32x4{y[0], y[1], y[2], y[3]}; }
 __device__ __forceinline__ void store_some(uint16_t *p, const float (&y)[4])
 {
@@ -601,12 +606,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         for (int r = 0; r < 4; ++r) {
             float *const to = sums + (wave * 16 + mine) * kStride + (c * 16 + quarter * 4 + r) * kEach;
 #pragma unroll
-            for (int e = 0; e < kEach; e += 4) {
-                f32x4 x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = o[c][e + i][r] * by;
-                *reinterpret_cast<f32x4 *>(to + e) = x;
-            }
+            for (int e = 0; e < kEach; e += 2) *reinterpret_cast<f32x2 *>(to + e) = f32x2{o[c][e][r] * by, o[c][e + 1][r] * by};
         }
     if (MODE != kAttendOwn && odd) add_odd_values<T, 16>(a, w, keys, BN, wave, 4, at, sums + wave * 16 * kStride, kStride, 0, a.dim);
     __syncthreads();
@@ -1200,8 +1200,13 @@ static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &
 template <class T>
 static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &p, dim3 grid)
 {
-    if (a.dim <= 64) launch_pieces<T, 64>(ctx, a, p, grid);
-    else if (a.dim <= 128) launch_pieces<T, 128>(ctx, a, p, grid);
+    if (a.dim <= 64) return launch_pieces<T, 64>(ctx, a, p, grid);
+    if constexpr (sizeof(T) == 4) {
+        // (fp32 products are bound by the matrix instructions: rows padded to less)
+        if (a.dim <= 96) return launch_pieces<T, 96>(ctx, a, p, grid);
+        if (a.dim > 128 && a.dim <= 192) return launch_pieces<T, 192>(ctx, a, p, grid);
+    }
+    if (a.dim <= 128) launch_pieces<T, 128>(ctx, a, p, grid);
     else launch_pieces<T, 256>(ctx, a, p, grid);
 }
 
