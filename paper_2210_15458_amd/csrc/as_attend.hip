@@ -1094,15 +1094,17 @@ __device__ __forceinline__ void attend_own(const AttendArgs &a, const AttendPiec
 }
 
 template <class T, int DP, bool FULL, bool BYPAGE>
-__global__ __launch_bounds__(256) void attend_own_kernel(AttendArgs a, AttendPieces p)
+__global__ __launch_bounds__(256, DP == 96 ? 3 : 1) void attend_own_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ RowsShared<T, DP> shared;
     attend_own<T, DP, FULL, BYPAGE>(a, p.piece[0], blockIdx.x, shared);
 }
 
 // Queries of prompts, or of rows that share a prompt (MODE) with what is the rows' own beside them: 16 a block, or 128.
+// (fp32 rows of up to 96 dimensions: three blocks a compute unit, for which the compiler has to save a few registers: prompts_f32_odd
+// 29.1 us with two, 24.5 with three)
 template <class T, int DP, bool FULL, bool BYPAGE, int MODE>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a, AttendPieces p)
+__global__ __launch_bounds__(256, DP == 96 ? 3 : 1) void attend_rows_kernel(AttendArgs a, AttendPieces p)
 {
     __shared__ RowsShared<T, DP> shared;
     uint32_t b = blockIdx.x, item;
