@@ -401,6 +401,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         const int32_t page = __shfl(at.page, 16 * s + x, kWave), token = at.base + 16 * s + x;
         return keys_at + (uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((token < keys.n ? token : keys.n - 1) & slots) * bytes);
     };
+    // (past a row's end its first piece stands in: the queries are zero there, and what comes out of the values is not stored)
     auto load_keys = [&](const Rows &at) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
@@ -432,23 +433,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             }
         }
     };
-    // what lies past the rows' ends
-    auto cut_keys = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kKey; ++i)
-#pragma unroll
-            for (int s = 0; s < kSub; ++s)
-                if (!FULL && (i * 4 + quarter) * 16 >= bytes) k[s][i] = u32x4{0, 0, 0, 0};
-    };
-    auto cut_values = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-            for (int e = 0; e < kSub * 4; ++e)
-#pragma unroll
-                for (int i = 0; i < kWords; ++i)
-                    if (!FULL && (c * 16 + mine) * kVBytes >= bytes) v[e][c][i] = 0;
-    };
     if (first < keys.last) {
         const Rows at = rows_at(keys.base(first, BN), ahead);
         ahead = find_pages(tile_base(first + WAVES));
@@ -458,7 +442,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
 #pragma unroll 1
     for (int32_t t = first; t < keys.last; t += WAVES) {
         const int32_t base = keys.base(t, BN);
-        cut_keys();
         // scores
         f32x4 s4[kSub];
 #pragma unroll
@@ -480,7 +463,6 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         const Rows next = rows_at(tile_base(t + WAVES), ahead);
         ahead = find_pages(tile_base(t + 2 * WAVES));
         load_keys(next);
-        cut_values();
         float p[kSub * 4];
 #pragma unroll
         for (int e = 0; e < kSub * 4; ++e) p[e] = s4[e >> 2][e & 3] * a.scale;
@@ -731,9 +713,6 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         shared.head[wave * 32 + mine] = w.qhead;
     }
     if (threadIdx.x == 0) any_odd = 0;
-    if (!FULL) {                                       // what lies past the rows' ends is never written to again
-        for (int i = threadIdx.x; i < 4 * F::kBytes / 16; i += 256) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
-    }
     const int32_t lo = w.lo, hi = w.hi, wave_lo = w.wave_lo, wave_hi = w.wave_hi;
     // the queries (zeros where there is none and past the row's end)
     u32x4 q[DP / 16];
@@ -749,22 +728,22 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         }
     }
     const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
-    if (!FULL) __syncthreads();
     const Keys keys = keys_of(a, w, lo, hi, BN, part, piece.parts, piece.least);
 
     // What a wave fetches of a tile: BN / 4 rows after each other (all in one page, of pages of 16 tokens and more), kLoads KiB, of which
     // a lane takes 16 bytes each, such that they land in their place.
     constexpr int kWaveRows = BN / 4;
     const int32_t row0 = wave * kWaveRows + lane / kPieces;           // (load i: i kRowsEach further on)
-    int32_t key_off[kLoads], value_off[kLoads];
+    int32_t key_off[kLoads], value_off;
+    const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
+    // (past a row's end its first piece stands in: the queries are zero there, and what comes out of the values is not stored)
+    auto piece_of = [&](int place) __attribute__((always_inline)) {
+        const int32_t at_byte = ((lane % kPieces) ^ place) * 16;
+        return in_rows + (FULL || at_byte < bytes ? at_byte : 0);
+    };
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int32_t row = row0 + i * F::kRowsEach;
-        // (full rows: load i's KiB lies i KiB behind the first both in memory and in LDS, which the instruction adds)
-        const int32_t in_rows = BYPAGE ? (lane / kPieces + (FULL ? 0 : i * F::kRowsEach)) * bytes : 0;
-        key_off[i] = in_rows + ((lane % kPieces) ^ F::key_place(row)) * 16;
-        value_off[i] = in_rows + ((lane % kPieces) ^ F::value_place(row)) * 16;
-    }
+    for (int i = 0; i < kLoads; ++i) key_off[i] = piece_of(F::key_place(row0 + i * F::kRowsEach));
+    value_off = piece_of(F::value_place(row0));        // (the same of all loads)
     const int32_t last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0, slots = (1 << a.page_shift) - 1;
     const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
     const char *const values_at = (const char *)a.v + ((int64_t)w.head << a.page_shift) * bytes;
@@ -785,17 +764,21 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     auto fetch = [&](int32_t base, const Pages &p, int buffer) __attribute__((always_inline)) {
         unsigned char *const to = smem + buffer * F::kBytes + wave * (kWaveRows * kRow);
         const char *const from = buffer < 2 ? keys_at : values_at;
-        const int32_t(&off)[kLoads] = buffer < 2 ? key_off : value_off;
+        auto off = [&](int i) __attribute__((always_inline)) { return buffer < 2 ? key_off[i] : value_off; };
         if constexpr (BYPAGE) {
             int32_t page = p.page[0] < 0 ? 0 : p.page[0];
             page = page < a.pages ? page : a.pages - 1;
             const char *const at = from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((base + wave * kWaveRows) & slots) * bytes));
             if constexpr (FULL) {
-                fetch_lds(at, off, to);
+                // (load i's KiB lies i KiB behind the first both in memory and in LDS, which the instruction adds)
+                int32_t offs[kLoads];
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) offs[i] = off(i);
+                fetch_lds(at, offs, to);
             } else {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
-                    if (off[i] - (lane / kPieces + i * F::kRowsEach) * bytes < bytes) fetch_lds(at, {off[i]}, to + i * 1024);
+                    fetch_lds(at + i * F::kRowsEach * bytes, {off(i)}, to + i * 1024);
             }
         } else {
 #pragma unroll
@@ -803,7 +786,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
                 const int32_t x = base + row0 + i * F::kRowsEach, there = x < keys.n ? x : keys.n - 1;
                 int32_t page = p.page[i] < 0 ? 0 : p.page[i];
                 page = page < a.pages ? page : a.pages - 1;
-                if (off[i] < bytes) fetch_lds(from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)((there & slots) * bytes + off[i])), to + i * 1024);
+                fetch_lds(from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)((there & slots) * bytes + off(i))), to + i * 1024);
             }
         }
     };
@@ -889,20 +872,20 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     };
     // One tile: its weights and their product with its values, under it the next tile's scores; the tile after that one's keys and
     // the next one's values are asked for.
-    Pages ahead;                                       // of the next tile ...
-    int32_t next_base = 0, after_base = 0;             // ... and where it and the one after it start
+    Pages next_pages, after_pages;                     // of the next tile and the one after it (a page a lane: looked up a step before)
+    auto pages_of = [&](int32_t t) __attribute__((always_inline)) { return find_pages(keys.base(t < keys.last ? t : keys.last - 1, BN)); };
     auto step = [&](int32_t t, int32_t base, int buffer, Scores &now, Scores &next) __attribute__((always_inline)) {
         tile_barrier();
         const bool more = t + 1 < keys.last;
-        if (more) {
-            next_base = keys.base(t + 1, BN);
-            fetch(next_base, ahead, 2 + (buffer ^ 1));
-        }
+        const int32_t next_base = keys.base(t + 1, BN);
+        if (more) fetch(next_base, next_pages, 2 + (buffer ^ 1));
         if (t + 2 < keys.last) {
-            after_base = keys.base(t + 2, BN);
-            ahead = find_pages(after_base);
-            fetch(after_base, ahead, buffer);
+            const int32_t after_base = keys.base(t + 2, BN);
+            if constexpr (BYPAGE) after_pages = find_pages(after_base);        // (by the scalar cache)
+            fetch(after_base, after_pages, buffer);
         }
+        next_pages = after_pages;
+        if constexpr (!BYPAGE) after_pages = pages_of(t + 3);
         unsigned char *const vs = smem + (2 + buffer) * F::kBytes;
         if (!(base <= block_whole && (base > block_from || base + BN <= keys.sinks))) {
             // what no query sees may be anything, and 0 * NaN is NaN; what is no number and seen by some alone is added at the end
@@ -962,27 +945,23 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     };
     if (keys.first < keys.last) {
         const int32_t base = keys.base(keys.first, BN);
-        ahead = find_pages(base);
-        fetch(base, ahead, 0);
-        fetch(base, ahead, 2);
-        if (keys.first + 1 < keys.last) {
-            next_base = keys.base(keys.first + 1, BN);
-            ahead = find_pages(next_base);
-        }
+        const Pages pages = find_pages(base);
+        next_pages = pages_of(keys.first + 1);
+        if constexpr (!BYPAGE) after_pages = pages_of(keys.first + 2);
+        fetch(base, pages, 0);
+        fetch(base, pages, 2);
         tile_barrier();
-        if (keys.first + 1 < keys.last) fetch(next_base, ahead, 1);
+        if (keys.first + 1 < keys.last) fetch(keys.base(keys.first + 1, BN), next_pages, 1);
         Scores one, two;
         score(smem, one, [](int) {});
         hide(base, one);
-        int32_t t = keys.first, at_base = base;
+        int32_t t = keys.first;
 #pragma unroll 1
         for (;;) {
-            step(t, at_base, 0, one, two);
+            step(t, keys.base(t, BN), 0, one, two);
             if (++t >= keys.last) break;
-            at_base = next_base;
-            step(t, at_base, 1, two, one);
+            step(t, keys.base(t, BN), 1, two, one);
             if (++t >= keys.last) break;
-            at_base = next_base;
         }
     }
 
@@ -1261,7 +1240,7 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
     p.every = 1;
     if (p.count == 2) {
         const int64_t first = (int64_t)p.piece[0].blocks * p.piece[0].parts, second = (int64_t)p.piece[1].blocks * p.piece[1].parts;
-        p.every = (uint32_t)(1 + second / (2 * first));
+        p.every = (uint32_t)(1 + second / (2 * first)) | 1;        // (odd: blocks go round eight XCDs, and so then do every so many of them)
         fits = fits && first + second <= 0x7fffffffLL;
     }
     // (and the queries' heads, where they are joined)
