@@ -734,7 +734,8 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     // a lane takes 16 bytes each, such that they land in their place.
     constexpr int kWaveRows = BN / 4;
     const int32_t row0 = wave * kWaveRows + lane / kPieces;           // (load i: i kRowsEach further on)
-    int32_t key_off[kLoads], value_off;
+    constexpr int kValueOffs = F::kRowsEach % 4 == 0 ? 1 : kLoads;        // (where a load's rows start the exchange anew, one for all)
+    int32_t key_off[kLoads], value_off[kValueOffs];
     const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
     // (past a row's end its first piece stands in: the queries are zero there, and what comes out of the values is not stored)
     auto piece_of = [&](int place) __attribute__((always_inline)) {
@@ -743,7 +744,8 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     };
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) key_off[i] = piece_of(F::key_place(row0 + i * F::kRowsEach));
-    value_off = piece_of(F::value_place(row0));        // (the same of all loads)
+#pragma unroll
+    for (int i = 0; i < kValueOffs; ++i) value_off[i] = piece_of(F::value_place(row0 + i * F::kRowsEach));
     const int32_t last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0, slots = (1 << a.page_shift) - 1;
     const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
     const char *const values_at = (const char *)a.v + ((int64_t)w.head << a.page_shift) * bytes;
@@ -764,7 +766,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     auto fetch = [&](int32_t base, const Pages &p, int buffer) __attribute__((always_inline)) {
         unsigned char *const to = smem + buffer * F::kBytes + wave * (kWaveRows * kRow);
         const char *const from = buffer < 2 ? keys_at : values_at;
-        auto off = [&](int i) __attribute__((always_inline)) { return buffer < 2 ? key_off[i] : value_off; };
+        auto off = [&](int i) __attribute__((always_inline)) { return buffer < 2 ? key_off[i] : value_off[i % kValueOffs]; };
         if constexpr (BYPAGE) {
             int32_t page = p.page[0] < 0 ? 0 : p.page[0];
             page = page < a.pages ? page : a.pages - 1;
