@@ -590,6 +590,9 @@ def _heads_of(cache, q):
     return heads, cols
 
 
+_MOST = 0x7fffffff
+
+
 def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
     """Attention of one query a row, q and out [rows, heads * head_dim] (or [rows, heads, head_dim]); scale: 1 / sqrt(head_dim)."""
     _one_device(ctx, cache, seqs)
@@ -597,7 +600,8 @@ def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
     rows = seqs.rows
     qp, ldq = _tokens_of(cache, q, "q", rows, cols)
     op, ldo = _tokens_of(cache, out, "out", rows, cols)
-    rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.scale if scale is None else scale, window, sinks, op, ldo)
+    rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.scale if scale is None else float(scale),
+                                   window if window < _MOST else _MOST, sinks if sinks < _MOST else _MOST, op, ldo)
     if rc:
         ctx._check(rc)
 
@@ -609,7 +613,7 @@ def as_attend_prompts(ctx, cache, seqs, q, offsets, out, scale=None, window=0, s
     n, at = q.size(0), _offsets_of(cache, seqs, offsets)
     qp, ldq = _tokens_of(cache, q, "q", n, cols)
     op, ldo = _tokens_of(cache, out, "out", n, cols)
-    rc = (_lib or lib()).as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, at, heads, cache.scale if scale is None else scale,
-                                           window, sinks, op, ldo)
+    rc = (_lib or lib()).as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, at, heads, cache.scale if scale is None else float(scale),
+                                           window if window < _MOST else _MOST, sinks if sinks < _MOST else _MOST, op, ldo)
     if rc:
         ctx._check(rc)

@@ -31,7 +31,7 @@ def run(batch, heads, window=0, sinks=0, scale=None, finished=None, pad=0, ctx=N
 
 @pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,kv_heads,group,page", [(64, 2, 4, 16), (128, 1, 1, 16), (128, 3, 8, 64), (256, 2, 2, 16), (8, 1, 3, 4), (72, 2, 5, 1),
-                                                     (136, 1, 16, 8), (96, 2, 17, 32), (128, 1, 33, 2), (200, 1, 4, 128), (64, 5, 1, 1024)])
+                                                     (136, 1, 16, 8), (96, 2, 17, 32), (128, 1, 33, 2), (200, 1, 4, 128), (192, 1, 4, 16), (104, 2, 2, 16), (64, 5, 1, 1024)])
 def test_lengths(dtype, dim, kv_heads, group, page):
     own = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 130, 257, 300]
     b = Batch(own, dim, kv_heads, page, dtype, seed=dim + group)
@@ -176,3 +176,23 @@ def test_same_bits_each_time_and_whatever_the_other_rows_are():
     other[0] = NAN
     _, three = run(b, 8, q=other)
     assert torch.equal(one[1:], three[1:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,kv_heads,group,page,room", [(64, 3, 4, 16, 64), (128, 8, 4, 16, 200), (72, 3, 3, 8, 90), (96, 2, 1, 16, 40), (256, 3, 2, 64, 300), (192, 2, 5, 1, 33),
+                                                          (128, 4, 20, 16, 500)])
+@pytest.mark.parametrize("prompts", [False, True])
+def test_many_short_rows(dtype, dim, kv_heads, group, page, room, prompts):
+    """So many that each is one wave's, with what its prompt left and without; some finished, some empty."""
+    rows = -(-2048 // kv_heads // 10) * 10 + 10
+    own = [(r * 37) % (room + 1) for r in range(rows)]
+    own[3] = room
+    b = Batch(own, dim, kv_heads, page, dtype, prompts=[0, 33, 70][:2] + [5] * (rows // 10 - 2) if prompts else None, per=10, seed=dim)
+    assert rows * kv_heads >= 2048 and b.table.shape[1] * page <= 512
+    finished = torch.zeros(rows, dtype=torch.uint8, device="cuda")
+    finished[7], finished[rows - 2] = 1, 1
+    keep = [0, 1, 2, 3, 11, 12, 19, 20, 55, rows // 2, rows - 1]
+    for window, sinks in ((0, 0), (11, 3)):
+        q, out = run(b, kv_heads * group, window=window, sinks=sinks, finished=finished, pad=2)
+        assert bool((out[[7, rows - 2]] == 7).all())
+        check(out, q, b, window=window, sinks=sinks, rows=keep)

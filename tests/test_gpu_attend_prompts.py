@@ -36,7 +36,7 @@ def run(batch, new, heads, window=0, sinks=0, finished=None, pad=0, before=0, be
 
 @pytest.mark.parametrize("dtype", FORMS)
 @pytest.mark.parametrize("dim,kv_heads,group,page", [(64, 2, 4, 16), (128, 1, 1, 16), (128, 2, 8, 64), (256, 1, 2, 16), (8, 1, 3, 4), (72, 2, 5, 1),
-                                                     (136, 1, 16, 8), (96, 1, 17, 32), (200, 1, 4, 128), (64, 3, 1, 1024)])
+                                                     (136, 1, 16, 8), (96, 1, 17, 32), (200, 1, 4, 128), (192, 1, 4, 16), (104, 2, 2, 16), (64, 3, 1, 1024)])
 def test_chunks(dtype, dim, kv_heads, group, page):
     new = [1, 0, 3, 33, 64, 0, 0, 17, 130, 1]
     had = [0, 5, 70, 0, 31, 0, 9, 200, 33, 299]
