@@ -1222,20 +1222,34 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         fits = fits && groups * tiles * x.parts <= 0x7fffffffLL;
         x.groups = (uint32_t)groups;
         x.items = x.blocks = (uint32_t)(groups * tiles);
-        // many short rows: one a wave
-        x.alone = mode == kAttendOwn && x.parts == 1 && room <= 512 && groups * tiles >= 8 * (int64_t)ctx->num_cus;
+        // Many short rows: one a wave, which spares them the joining of four.  us in blocks / in waves, 4 heads of 128, bf16: 512 of them
+        // of up to 256 tokens 13.5 / 14.4; 1024 of up to 32, 128, 256, 512 9.3 / 5.9, 17.4 / 12.3, 24 / 20, 36 / 34; 2048 19 / 8.8, 30 / 20,
+        // 41 / 36, 78 / 78; 8192 69 / 32, 121 / 88, 175 / 160, 291 / 297; fp32 1024 13 / 7.9, 26 / 20, 40 / 35, 78 / 77.
+        x.alone = mode == kAttendOwn && x.parts == 1 && room <= 256 && groups * tiles >= 4 * (int64_t)ctx->num_cus;
         if (x.alone) x.blocks = (x.items + 3) / 4;
     };
-    // many queries that share a key head: by tiles of 128
-    const bool bf16 = a.dtype == AS_BF16;
+    // Queries that share a key head, 16 or 128 a block (bf16): 128 take more time to start and less a query.  They pay where the 16s
+    // are more blocks than the GPU takes at once, or read the keys too often: us for 16 / 128, dim 128, prompts of 1024 that rows of 32
+    // queries share 2 of them 11.7 / 14.8, 16 of them 22.0 / 22.1, of 64 queries 36 / 24; of 8192 and 64 queries 131 / 69, 16 queries
+    // 50 / 52; of 128 and 64 20 / 17; chunks of 16 queries behind 2000 tokens 4 of them 14 / 17, 64 of them 75 / 53; whole prompts of
+    // 16, 32, 64, 256 queries, 64 of them, 7.3 / 8.3, 11.5 / 8.8, 16 / 9.6, 52 / 19.
+    // (reads: blocks of 16 queries times the keys that each may have)
+    auto by_128 = [&](int64_t blocks, int64_t most_blocks, double reads, int most_log) {
+        if (a.dtype != AS_BF16 || ctx->attend_shape == 1) return false;
+        return ctx->attend_shape == 2 || blocks > most_blocks || reads * a.dim >= (double)(1 << most_log);
+    };
     if (a.offsets) {
-        const int queries = bf16 && ctx->attend_shape != 1 && (ctx->attend_shape == 2 || a.tokens * a.group >= 32 * a.rows) ? 128 : 16;
-        add(kAttendRagged, queries, (a.tokens * a.group / queries + a.rows) * a.kv_heads, 1, a.room);
+        const int64_t all = a.tokens * a.group;
+        const bool many = (all >= 16 * a.rows || ctx->attend_shape == 2) &&
+                          by_128((all / 16 + a.rows) * a.kv_heads, 2 * (int64_t)ctx->num_cus, (double)all / 16 * a.kv_heads * a.room, 25);
+        const int queries = many ? 128 : 16;
+        add(kAttendRagged, queries, (all / queries + a.rows) * a.kv_heads, 1, a.room);
     } else {
         if (a.prompt_table) {
-            const int64_t all = a.per * (int64_t)a.group;
-            const int queries = bf16 && ctx->attend_shape != 1 && (ctx->attend_shape == 2 || all >= 32) ? 128 : 16;
-            add(kAttendShared, queries, (a.rows + a.per - 1) / a.per * a.kv_heads, (int32_t)((all + queries - 1) / queries), a.prompt_room);
+            const int64_t all = a.per * (int64_t)a.group, groups = (a.rows + a.per - 1) / a.per * a.kv_heads;
+            const bool many = (all > 16 || ctx->attend_shape == 2) && by_128(groups * ((all + 15) / 16), (int64_t)ctx->num_cus - 1, (double)groups * ((all + 15) / 16) * a.prompt_room, 24);
+            const int queries = many ? 128 : 16;
+            add(kAttendShared, queries, groups, (int32_t)((all + queries - 1) / queries), a.prompt_room);
         }
         if (a.table) add(kAttendOwn, 16, a.rows * a.kv_heads, (a.group + 15) / 16, a.room);
     }
