@@ -679,13 +679,17 @@ as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *s
  * the cache's dtype.
  *   q, out     DEVICE [rows, heads, head_dim], the cache's dtype, rows ldq and ldo >=
  *              heads * head_dim apart; may start anywhere
+ *              out must not overlap q, k or v
  *   heads      a multiple of kv_heads, at most AS_MAX_HEADS
+ *   scale      finite (usually 1 / sqrt(head_dim))
  * The keys are split over the GPU where there are few rows, and those of prompts
  * taken for all their rows together: what the parts come to lies in a workspace of
  * the context, which is (re)allocated when a call needs more than any earlier one
  * did; that call synchronises the stream, frees what graphs captured earlier work
  * on, and must not be made under capture.  What a call needs goes by its sizes
- * alone (rows, heads, head_dim, the tables' widths), not by lengths.
+ * alone (rows, heads, head_dim, dtype, the tables' widths, page_size), not by
+ * lengths; few rows may need more than many.  AS_ERR_UNSUPPORTED where a prompt's
+ * queries, or all blocks, do not fit 31 bits.
  * The same call gives the same bits each time; rows do not affect each other.
  */
 as_status as_attend(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
