@@ -365,9 +365,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         for (int i = 0; i < kKey; ++i) {
             const int32_t o = (i * 4 + quarter) * 16;
             q[i] = u32x4{0, 0, 0, 0};
-            if (w.valid && (FULL || o < bytes)) q[i] = *reinterpret_cast<const u32x4_any *>(from + o);
+            if (w.valid && a.scale != 0.f && (FULL || o < bytes)) q[i] = *reinterpret_cast<const u32x4_any *>(from + o);
+            if (a.scale < 0.f) q[i] ^= kBf16 ? 0x80008000u : 0x80000000u;
         }
     }
+    const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
     f32x4 o[kChunks][kEach];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
@@ -450,6 +452,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
             s4[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // fp32: four sums, which stay smaller than one, and so their roundings (256 dimensions: errors against 64 bits 1.0e-6 in one
+            // sum, below 6e-7 in four; the same time)
+            f32x4 chains[4] = {s4[s], s4[s], s4[s], s4[s]};
 #pragma unroll
             for (int i = 0; i < kKey; ++i) {
                 if constexpr (kBf16) {
@@ -457,10 +462,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        s4[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[s][i][e]),
-                                                                     __builtin_bit_cast(float, (uint32_t)q[i][e]), s4[s], 0, 0, 0);
+                        chains[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[s][i][e]),
+                                                                         __builtin_bit_cast(float, (uint32_t)q[i][e]), chains[e], 0, 0, 0);
                 }
             }
+            if constexpr (!kBf16) s4[s] = (chains[0] + chains[1]) + (chains[2] + chains[3]);
         }
         // the next tile's keys take their registers, and its values theirs behind this tile's
         const Rows next = rows_at(tile_base(t + WAVES), ahead);
@@ -468,7 +474,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         load_keys(next);
         float p[kSub * 4];
 #pragma unroll
-        for (int e = 0; e < kSub * 4; ++e) p[e] = s4[e >> 2][e & 3] * a.scale;
+        for (int e = 0; e < kSub * 4; ++e) p[e] = s4[e >> 2][e & 3];
         if (!keys.whole(base, BN)) {
             uint32_t largest = 0;
 #pragma unroll
@@ -503,6 +509,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         for (int e = 1; e < kSub * 4; ++e) top = fmaxf(top, p[e]);
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        top = top == kNone ? kNone : top * scale;
         if (__any(top > m)) {
             const float now = fmaxf(top, m);
             const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f(m - now);
@@ -515,7 +522,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         }
         const float ref = m == kNone ? 0.f : m;
 #pragma unroll
-        for (int e = 0; e < kSub * 4; ++e) p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+        for (int e = 0; e < kSub * 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], scale, -ref));
         if constexpr (kBf16) {
             // Weights go into the product as bf16; l adds up the rounded ones, so that they come to 1 all the same.
             u32x4 pw;

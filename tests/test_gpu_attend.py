@@ -196,3 +196,10 @@ def test_many_short_rows(dtype, dim, kv_heads, group, page, room, prompts):
         q, out = run(b, kv_heads * group, window=window, sinks=sinks, finished=finished, pad=2)
         assert bool((out[[7, rows - 2]] == 7).all())
         check(out, q, b, window=window, sinks=sinks, rows=keep)
+
+
+@pytest.mark.parametrize("dtype", FORMS)
+def test_a_thousand_heads_on_one(dtype):
+    b = Batch([70, 3], 8, 1, 16, dtype, prompts=[40], per=2, seed=7)
+    q, out = run(b, 1024)
+    check(out, q, b)

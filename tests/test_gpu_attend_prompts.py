@@ -172,3 +172,10 @@ def test_offsets_out_of_range_are_not_followed():
     torch.cuda.synchronize()
     B.as_attend_prompts(ctx, B.Cache(b.k, b.v), B.Sequences(3, b.table, b.lens), q, torch.tensor([0, 40, 70, 90], device="cuda"), out)
     check(out, q, b, offsets=[0, 40, 70, 90])
+
+
+@pytest.mark.parametrize("dtype", FORMS)
+def test_a_thousand_heads_on_one(dtype):
+    b = Batch([9, 40], 8, 1, 16, dtype, seed=7)
+    q, out, offsets = run(b, [2, 3], 1024)
+    check(out, q, b, offsets=offsets)
