@@ -679,9 +679,9 @@ __device__ __forceinline__ void fetch_lds(const char *base, const int32_t (&offs
                      "s"(base), "v"(offset[0]), "v"(offset[1])
                      : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072" ::"s"(at),
-                     "s"(base), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3])
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:%6\n\t"
+                     "global_load_lds_dwordx4 %4, %1 offset:%7\n\tglobal_load_lds_dwordx4 %5, %1 offset:%8" ::"s"(at),
+                     "s"(base), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "n"(1 << 10), "n"(2 << 10), "n"(3 << 10)
                      : "memory");
 }
 __device__ __forceinline__ void fetch_lds(const char *from, unsigned char *to)
@@ -1096,8 +1096,8 @@ __global__ __launch_bounds__(256, DP == 96 ? 3 : 1) void attend_own_kernel(Atten
 }
 
 // Queries of prompts, or of rows that share a prompt (MODE) with what is the rows' own beside them: 16 a block, or 128.
-// (fp32 rows of up to 96 dimensions: three blocks a compute unit, for which the compiler has to save a few registers: prompts_f32_odd
-// 29.1 us with two, 24.5 with three)
+// (fp32 rows of up to 96 dimensions: three blocks a compute unit, for which the compiler has to save a few registers: nine chunks of up
+// to 301 tokens behind up to 77, 6 heads of 72 over 2, 29.1 us with two, 24.5 with three)
 template <class T, int DP, bool FULL, bool BYPAGE, int MODE>
 __global__ __launch_bounds__(256, DP == 96 ? 3 : 1) void attend_rows_kernel(AttendArgs a, AttendPieces p)
 {
