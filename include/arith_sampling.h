@@ -691,7 +691,9 @@ as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *s
  * alone (rows, heads, head_dim, dtype, the tables' widths, page_size), not by
  * lengths; few rows may need more than many.  AS_ERR_UNSUPPORTED where a prompt's
  * queries, or all blocks, do not fit 31 bits.
- * The same call gives the same bits each time; rows do not affect each other.
+ * The same call gives the same bits each time.  What a row asks for and has in the cache does not
+ * affect other rows: not a bit of theirs without a window; with one, how many tokens of their
+ * own the other rows of a prompt have, and which are finished, may change the order of a row's sums.
  */
 as_status as_attend(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
                     int64_t rows, const void *q, int64_t ldq, int32_t heads, float scale,

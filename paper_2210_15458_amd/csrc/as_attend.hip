@@ -932,9 +932,10 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         top = halves_max(top);
         top = top == kNone ? kNone : top * scale;
         if (__any(top > m + 8.f)) {
-            const float up = fmaxf(top, m);
-            const float by = up == kNone ? 1.f : __builtin_amdgcn_exp2f(m - up);
-            m = up;
+            // (each query by its own scores alone: what a neighbour asks for is not to change its bits)
+            const bool raised = top > m + 8.f;
+            const float by = raised ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+            m = raised ? top : m;
             l *= by;
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) o[i] *= by;
