@@ -299,6 +299,10 @@ template <int DP> struct AttendForm<float, DP> {
     static constexpr int kSub = 1, kKey = DP / 16, kVBytes = DP == 96 ? 8 : 16, kEach = kVBytes / 4, kChunks = DP / (16 * kEach);
 };
 
+// Of the dimensions that come to a form of DP the fewest: which of a row's pieces may lie past its end.
+template <class T, int DP>
+constexpr int kLeastDim = DP == 64 ? 8 : sizeof(T) == 2 ? DP / 2 + 8 : DP == 96 ? 72 : DP == 128 ? 104 : DP == 192 ? 136 : 200;
+
 // Two, four or eight values after each other.
 __device__ __forceinline__ void store_some(float *p, const float (&y)[2])
 {
@@ -406,7 +410,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         const int32_t page = __shfl(at.page, 16 * s + x, kWave), token = at.base + 16 * s + x;
         return keys_at + (uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)(((token < keys.n ? token : keys.n - 1) & slots) * bytes);
     };
-    // (past a row's end its first piece stands in: the queries are zero there, and what comes out of the values is not stored)
+    // (past a row's end its first piece stands in: of keys it is made zeros before the product, since the queries' zeros are not enough
+    // where it holds an infinity; what comes out of the values is not stored)
     auto load_keys = [&](const Rows &at) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
@@ -457,6 +462,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             f32x4 chains[4] = {s4[s], s4[s], s4[s], s4[s]};
 #pragma unroll
             for (int i = 0; i < kKey; ++i) {
+                if (!FULL && (i * 4 + 3) * 16 >= kLeastDim<T, DP> * (int)sizeof(T) && (i * 4 + quarter) * 16 >= bytes) k[s][i] = u32x4{0, 0, 0, 0};
                 if constexpr (kBf16) {
                     s4[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[s][i]), __builtin_bit_cast(bf16x8, q[i]), s4[s], 0, 0, 0);
                 } else {
@@ -695,6 +701,8 @@ __device__ __forceinline__ void tile_barrier()
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+__device__ const u32x4 kZeros = {0, 0, 0, 0};             // what stands in for keys past a row's end
+
 template <int DP> struct TilesShared {
     __attribute__((aligned(1024))) unsigned char smem[TileForm<DP>::kLds];
     int64_t token[TileForm<DP>::kQueries];             // of each query, -1: none ...
@@ -751,15 +759,18 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     constexpr int kValueOffs = F::kRowsEach % 4 == 0 ? 1 : kLoads;        // (where a load's rows start the exchange anew, one for all)
     int32_t key_off[kLoads], value_off[kValueOffs];
     const int32_t in_rows = BYPAGE ? lane / kPieces * bytes : 0;
-    // (past a row's end its first piece stands in: the queries are zero there, and what comes out of the values is not stored)
-    auto piece_of = [&](int place) __attribute__((always_inline)) {
+    // (past a row's end zeros from elsewhere stand in for keys, below 0 here: the queries' own would not do where what stands in holds
+    // an infinity; and the row's first piece for values: what comes out of them there is not stored.  2 chunks of up to 1072 queries, 16
+    // heads of 168 on one: 58.0 us with the row's first piece for keys too, 58.7 so, 61 with zeros put in as keys are read from LDS, 64.5
+    // with those lanes' requests left out; 6 of up to 362, 40 heads of 80, window 23: 24.9, 26.6, 26.7, 31.3)
+    auto piece_of = [&](int place, int32_t stand_in) __attribute__((always_inline)) {
         const int32_t at_byte = ((lane % kPieces) ^ place) * 16;
-        return in_rows + (FULL || at_byte < bytes ? at_byte : 0);
+        return FULL || at_byte < bytes ? in_rows + at_byte : stand_in;
     };
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) key_off[i] = piece_of(F::key_place(row0 + i * F::kRowsEach));
+    for (int i = 0; i < kLoads; ++i) key_off[i] = piece_of(F::key_place(row0 + i * F::kRowsEach), -1);
 #pragma unroll
-    for (int i = 0; i < kValueOffs; ++i) value_off[i] = piece_of(F::value_place(row0 + i * F::kRowsEach));
+    for (int i = 0; i < kValueOffs; ++i) value_off[i] = piece_of(F::value_place(row0 + i * F::kRowsEach), in_rows);
     const int32_t last_page = keys.n > 0 ? (keys.n - 1) >> a.page_shift : 0, slots = (1 << a.page_shift) - 1;
     const char *const keys_at = (const char *)a.k + ((int64_t)w.head << a.page_shift) * bytes;
     const char *const values_at = (const char *)a.v + ((int64_t)w.head << a.page_shift) * bytes;
@@ -793,8 +804,10 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
                 fetch_lds(at, offs, to);
             } else {
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-                    fetch_lds(at + i * F::kRowsEach * bytes, {off(i)}, to + i * 1024);
+                for (int i = 0; i < kLoads; ++i) {
+                    if (buffer < 2) fetch_lds(off(i) < 0 ? (const char *)&kZeros : at + (i * F::kRowsEach * bytes + off(i)), to + i * 1024);
+                    else fetch_lds(at + i * F::kRowsEach * bytes, {off(i)}, to + i * 1024);
+                }
             }
         } else {
 #pragma unroll
@@ -802,7 +815,8 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
                 const int32_t x = base + row0 + i * F::kRowsEach, there = x < keys.n ? x : keys.n - 1;
                 int32_t page = p.page[i] < 0 ? 0 : p.page[i];
                 page = page < a.pages ? page : a.pages - 1;
-                fetch_lds(from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)((there & slots) * bytes + off(i))), to + i * 1024);
+                const char *const at = from + ((uint64_t)(uint32_t)page * a.page_bytes + (uint32_t)((there & slots) * bytes + off(i)));
+                fetch_lds(!FULL && off(i) < 0 ? (const char *)&kZeros : at, to + i * 1024);
             }
         }
     };
