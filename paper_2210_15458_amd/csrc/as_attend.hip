@@ -18,6 +18,11 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNone = -__builtin_inff();
 
+// Scores are products until they are weighed: a weight is 2^((q.k - m) scale), m the largest q.k (of a negative scale's negated queries),
+// with log2(e) in the scale.  The difference is taken first: of a score times the scale and a rounded maximum times the scale what is
+// left is the product's rounding, which passes 2^127 where scores do 2^31.
+__device__ __forceinline__ float weight_scale(const AttendArgs &a) { return a.scale == 0.f ? 1.f : fabsf(a.scale); }      // (above 0; 0: the queries are zeros)
+
 // Two weights as bf16.  (By the compiler, not the instruction by hand: what an exponential has just left may be read by other
 // instructions only after a pause that the compiler sees to.)
 __device__ __forceinline__ uint32_t weights2(float lo, float hi)
@@ -373,7 +378,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
             if (a.scale < 0.f) q[i] ^= kBf16 ? 0x80008000u : 0x80000000u;
         }
     }
-    const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
+    const float scale = weight_scale(a);
     f32x4 o[kChunks][kEach];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
@@ -515,10 +520,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         for (int e = 1; e < kSub * 4; ++e) top = fmaxf(top, p[e]);
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        top = top == kNone ? kNone : top * scale;
         if (__any(top > m)) {
             const float now = fmaxf(top, m);
-            const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            const float by = now == kNone ? 1.f : __builtin_amdgcn_exp2f((m - now) * scale);
             m = now;
             l *= by;
 #pragma unroll
@@ -528,7 +532,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         }
         const float ref = m == kNone ? 0.f : m;
 #pragma unroll
-        for (int e = 0; e < kSub * 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], scale, -ref));
+        for (int e = 0; e < kSub * 4; ++e) p[e] = __builtin_amdgcn_exp2f((p[e] - ref) * scale);
         if constexpr (kBf16) {
             // Weights go into the product as bf16; l adds up the rounded ones, so that they come to 1 all the same.
             u32x4 pw;
@@ -597,7 +601,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
     float M = kNone;
 #pragma unroll
     for (int i = 0; i < 4; ++i) M = fmaxf(M, stats[i][mine].x);
-    const float by = m == kNone ? 0.f : __builtin_amdgcn_exp2f(m - M);
+    const float by = m == kNone ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale);
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
@@ -619,7 +623,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
         for (int j = 0; j < 4; ++j) top = fmaxf(top, stats[j][r].x);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (stats[j][r].x != kNone) total += stats[j][r].y * __builtin_amdgcn_exp2f(stats[j][r].x - top);
+            if (stats[j][r].x != kNone) total += stats[j][r].y * __builtin_amdgcn_exp2f((stats[j][r].x - top) * scale);
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
@@ -749,7 +753,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
             q[i] ^= sign;
         }
     }
-    const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale);        // (above 0: the largest product has the largest score)
+    const float scale = weight_scale(a);
     const Keys keys = keys_of(a, w, lo, hi, BN, part, piece.parts, piece.least);
 
     // What a wave fetches of a tile: BN / 4 rows after each other (all in one page, of pages of 16 tokens and more), kLoads KiB, of which
@@ -827,6 +831,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float m = kNone, l = 0.f;
+    // A weight by one instruction less, 2^(s scale - ref), ref = m scale rounded, where the rounding is far from mattering: sums are then
+    // relative to 2^ref, and `rest` is what m scale is beyond it, for where they meet others.
+    constexpr float kFar = 1 << 16;
+    const float slack = fminf(8.f / scale, 0x1.fffffep127f);
+    auto rest = [&](float x) __attribute__((always_inline)) {
+        const float ref = x * scale;
+        return fabsf(ref) < kFar ? fmaf(x, scale, -ref) : 0.f;
+    };
     typedef f32x16 Scores[BN / 32];
     const int kx = (half ^ F::key_place(mine)) * 16;
     const int32_t vrow = 4 * half + (lane & 15) / 4;
@@ -944,17 +956,24 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, now[b][r]);
         top = halves_max(top);
-        top = top == kNone ? kNone : top * scale;
-        if (__any(top > m + 8.f)) {
+        if (__any(top > m + slack)) {
             // (each query by its own scores alone: what a neighbour asks for is not to change its bits)
-            const bool raised = top > m + 8.f;
-            const float by = raised ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+            const bool raised = top > m + slack;
+            const float by = raised ? __builtin_amdgcn_exp2f(fmaf(m - top, scale, rest(top) - rest(m))) : 1.f;
             m = raised ? top : m;
             l *= by;
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) o[i] *= by;
         }
-        const float ref = m == kNone ? 0.f : m;
+        float ref = m == kNone ? 0.f : m * scale;
+        const bool far = fabsf(ref) >= kFar;
+        if (__any(far)) {
+            ref = far ? 0.f : ref;
+#pragma unroll
+            for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) now[b][r] = far ? now[b][r] - m : now[b][r];
+        }
         u32x4 pw[BN / 16];
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
@@ -999,10 +1018,11 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
     // sums to memory, 64 dimensions of a wave's queries at a time through its part of LDS
     l += __shfl_xor(l, 32, kWave);
     if (l != l && m == kNone) m = 0.f;
+    const float by = a.parts > 1 ? __builtin_amdgcn_exp2f(-rest(m)) : l > 0.f || l != l ? 1.f / l : 0.f;
+    l *= by;
     __syncthreads();
     const bool odd = any_odd != 0;
     float *const sums = reinterpret_cast<float *>(smem) + wave * 32 * kStride;
-    const float by = a.parts > 1 ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
     for (int c = 0; c < DP / 64; ++c) {
         if (c * 64 >= a.dim) break;
@@ -1162,7 +1182,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     const float2 *const stats = a.stats + (int64_t)i * a.parts;
     const float2 mine = lane < a.parts ? stats[lane] : float2{kNone, 0.f};
     const float M = wave_max(mine.x);
-    const float weight = mine.x == kNone ? 0.f : __builtin_amdgcn_exp2f(mine.x - M);
+    const float weight = mine.x == kNone ? 0.f : __builtin_amdgcn_exp2f((mine.x - M) * weight_scale(a));
     const float total = wave_sum(weight * mine.y);
     const float inverse = total > 0.f || total != total ? 1.f / total : 0.f;
     const uint64_t there = __ballot(mine.x != kNone);

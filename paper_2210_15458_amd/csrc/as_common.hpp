@@ -387,7 +387,7 @@ struct AttendArgs {
     int64_t tokens;              // queries
     const int64_t *offsets;      // [rows + 1] whose they are, or null: one a row
     float *sums;                 // [tokens, heads, parts, dim] where there are parts to join ...
-    float2 *stats;               // [tokens, heads, parts] ... and their largest scores and sums of weights
+    float2 *stats;               // [tokens, heads, parts] ... and their largest products q.k and sums of weights
     int32_t parts;
 };
 enum AttendMode { kAttendOwn, kAttendShared, kAttendRagged };
