@@ -1294,7 +1294,8 @@ static as_status check_queries(as_ctx *ctx, AttendArgs *a, const void *q, int64_
     if (!aligned_to(q, a->dtype) || !aligned_to(out, a->dtype)) return fail(ctx, AS_ERR_INVALID_ARG, "q or out is not aligned to its element type");
     a->q = q; a->ldq = ldq; a->out = out; a->ldo = ldo; a->heads = heads; a->group = heads / a->kv_heads;
     a->scale = scale * 1.44269504088896340736f;
-    a->window = window > 0 ? window : 0;
+    // (as wide as the tables' rooms is none; one that is left fits 32 bits when it is taken off any position)
+    a->window = window > 0 && window < (int64_t)a->prompt_room + a->room ? window : 0;
     a->sinks = sinks;
     return AS_OK;
 }

@@ -110,7 +110,8 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
         const uint32_t left = all - first < ROWS ? (uint32_t)(all - first) : ROWS;
         w.valid = mine < left;
         const uint32_t x = rest + (w.valid ? mine : left - 1), i = by_group(x);
-        const int32_t first_at = len - (int32_t)(f.to - f.from) + (int32_t)first_token;
+        int32_t first_at = len - (int32_t)(f.to - f.from) + (int32_t)first_token;
+        first_at = first_at > -ROWS ? first_at : -ROWS;        // (below 0 the item's queries see nothing, however far; and a window off it fits 32 bits)
         w.token = f.from + first_token + i;
         w.qhead = (int32_t)(w.head * G + x - i * G);
         w.at = first_at + (int32_t)i;
@@ -181,6 +182,7 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, const AttendPiece
             w.hi = __builtin_amdgcn_readfirstlane(w.hi);
         }
         if (w.lo > w.hi) w.lo = w.hi;                  // (no query)
+        if (w.wave_lo > w.wave_hi) w.wave_lo = w.wave_hi;
     }
     return true;
 }
@@ -885,7 +887,8 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const AttendPi
         if (base <= wave_whole && (base > wave_from || base + BN <= keys.sinks)) return;
         const int32_t first = base + 4 * half, upto = (at < keys.n ? at : keys.n - 1) - first;      // (of the tile's tokens, as the lane has them)
         if (a.window > 0) {
-            const int32_t from = at - a.window - first, sinks = keys.sinks - first;
+            // (unsigned, since a query before the tile's first may pass -2^31 here: it sees none of it whatever comes out)
+            const int32_t from = (int32_t)((uint32_t)at - (uint32_t)a.window - (uint32_t)first), sinks = keys.sinks - first;
 #pragma unroll
             for (int b = 0; b < BN / 32; ++b)
 #pragma unroll

@@ -373,7 +373,7 @@ struct AttendArgs {
     int32_t heads, group;        // group: of a key head
     uint32_t group_inverse;      // 2^24 / group, rounded up
     float scale;                 // times log2(e)
-    int32_t window, sinks;       // window <= 0: none
+    int32_t window, sinks;       // window 0: none; otherwise less than there is room for
     int64_t rows;                // sequences
     const int32_t *table;        // [rows, table_ld] pages, or null: no tokens of the rows' own
     int64_t table_ld;
