@@ -662,7 +662,8 @@ typedef struct as_sequences {
  *   offsets    DEVICE int64[rows + 1], not falling, or NULL (then tokens = rows)
  * Tokens that the table has no room for, and those before offsets[0] or from
  * offsets[rows] on, are left out.  No two rows may have a page in common that both
- * write to.  Allocates nothing.
+ * write to.  AS_ERR_UNSUPPORTED where a launch would need more than 2^24 - 1 work-groups (one
+ * for the tokens that fill it, and with offsets one a row).  Allocates nothing.
  */
 as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *sequences,
                        int64_t rows, const void *k, int64_t ldk, const void *v, int64_t ldv,
@@ -690,7 +691,8 @@ as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *s
  * on, and must not be made under capture.  What a call needs goes by its sizes
  * alone (rows, heads, head_dim, dtype, the tables' widths, page_size), not by
  * lengths; few rows may need more than many.  AS_ERR_UNSUPPORTED where a prompt's
- * queries, or all blocks, do not fit 31 bits.
+ * queries do not fit 31 bits, or a launch would need more than 2^24 - 1 work-groups (one
+ * a row and key head, or for four of them where they are many and short).
  * The same call gives the same bits each time.  What a row asks for and has in the cache does not
  * affect other rows: not a bit of theirs without a window; with one, how many tokens of their
  * own the other rows of a prompt have, and which are finished, may change the order of a row's sums.

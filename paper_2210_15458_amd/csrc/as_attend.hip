@@ -1246,6 +1246,9 @@ static void launch_pieces(as_ctx *ctx, const AttendArgs &a, const AttendPieces &
     else launch_pieces<T, 256>(ctx, a, p, grid);
 }
 
+// Blocks of 256 threads that a launch takes: its threads are counted in 32 bits.
+constexpr int64_t kMostBlocks = 0xffffffffLL / 256;
+
 // Parts that the keys of each query are split into: two blocks a compute unit, if each still has `least` keys.  Joining costs all
 // queries a pass over their parts, and prompts have many: they are split only where half of the units would have no block
 // (8192 tokens in 416 blocks: 16 us whole, 37 in two parts; 1024 rows over shared prompts of 512 21 whole, 18 in two, 23 in four).
@@ -1261,7 +1264,7 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
 {
     AttendPieces p{};
     *parts = 0;
-    // (a sequence's or a prompt's queries, and the blocks, in 32 bits)
+    // (a sequence's or a prompt's queries in 32 bits, and the blocks as a launch takes them)
     bool fits = a.tokens * a.group <= 0x7fffffffLL - 128 && a.per * (int64_t)a.group <= 0x7fffffffLL - 128;
     auto add = [&](int mode, int queries, int64_t groups, int32_t tiles, int64_t room) {
         AttendPiece &x = p.piece[p.count++];
@@ -1272,7 +1275,7 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         x.part0 = *parts;
         x.parts = parts_for(ctx, mode, groups * tiles, room, 256);
         *parts += x.parts;
-        fits = fits && groups * tiles * x.parts <= 0x7fffffffLL;
+        fits = fits && groups * tiles <= 0x7fffffffLL;
         x.groups = (uint32_t)groups;
         x.items = x.blocks = (uint32_t)(groups * tiles);
         // Many short rows: one a wave, which spares them the joining of four.  us in blocks / in waves, 4 heads of 128, bf16: 512 of them
@@ -1280,6 +1283,7 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
         // 41 / 36, 78 / 78; 8192 69 / 32, 121 / 88, 175 / 160, 291 / 297; fp32 1024 13 / 7.9, 26 / 20, 40 / 35, 78 / 77.
         x.alone = mode == kAttendOwn && x.parts == 1 && room <= 256 && groups * tiles >= 4 * (int64_t)ctx->num_cus;
         if (x.alone) x.blocks = (x.items + 3) / 4;
+        fits = fits && (int64_t)x.blocks * x.parts <= kMostBlocks;
     };
     // Queries that share a key head, 16 or 128 a block (bf16): 128 take more time to start and less a query.  They pay where the 16s
     // are more blocks than the GPU takes at once, or read the keys too often: us for 16 / 128, dim 128, prompts of 1024 that rows of 32
@@ -1310,10 +1314,10 @@ static AttendPieces pieces_of(const as_ctx *ctx, const AttendArgs &a, int32_t *p
     if (p.count == 2) {
         const int64_t first = (int64_t)p.piece[0].blocks * p.piece[0].parts, second = (int64_t)p.piece[1].blocks * p.piece[1].parts;
         p.every = (uint32_t)(1 + second / (2 * first)) | 1;        // (odd: blocks go round eight XCDs, and so then do every so many of them)
-        fits = fits && first + second <= 0x7fffffffLL;
+        fits = fits && first + second <= kMostBlocks;
     }
-    // (and the queries' heads, where they are joined)
-    *fit = fits && (*parts < 2 || a.tokens * a.heads <= 0x7fffffffLL);
+    // (and the queries' heads, where they are joined, four a block)
+    *fit = fits && (*parts < 2 || a.tokens * a.heads <= 4 * kMostBlocks);
     return p;
 }
 
@@ -1395,7 +1399,7 @@ as_status launch_cache_add(as_ctx *ctx, const AttendArgs &a, const void *k, int6
     int32_t each = (a.offsets ? 2048 : 256) / pieces;
     each = each < 1 ? 1 : each > 64 ? 64 : each;
     const int64_t blocks = a.offsets ? a.tokens / each + a.rows : (a.tokens + each - 1) / each;
-    if (blocks > 0x7fffffffLL) return fail(ctx, AS_ERR_UNSUPPORTED, "more tokens than one launch takes");
+    if (blocks > kMostBlocks) return fail(ctx, AS_ERR_UNSUPPORTED, "more tokens than one launch takes");
     hipLaunchKernelGGL(cache_add_kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a, k, ldk, v, ldv, each, esz);
     AS_HIP_TRY(ctx, hipGetLastError());
     return AS_OK;
