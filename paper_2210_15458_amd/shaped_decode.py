@@ -44,10 +44,15 @@ class Grammar:
 
 class Attention:
     """Blocks x + Wo attend(Wqkv x), a cache of pages each, for B prompts of up to prompt_room tokens and N rows each of up to
-    room tokens of their own.  blocks: pairs (Wqkv [(heads + 2 kv_heads) * dim, d], Wo [d, heads * dim])."""
+    room tokens of their own.  blocks: pairs (Wqkv [(heads + 2 kv_heads) * dim, d], Wo [d, heads * dim]).
+
+    step may be captured and replayed, with start between the replays: prompts have a context of their own, since what their
+    sizes need of its workspace (a short prompt more than a long one) must not move the one that a captured step works on.  A row takes
+    room steps; the tokens of further ones are not kept."""
 
     def __init__(self, ctx, blocks, heads, kv_heads, B_, N, prompt_room, room, finished, page=16, window=0, sinks=0):
-        self.ctx, self.finished, self.window, self.sinks = ctx, finished, window, sinks
+        self.ctx, self.finished, self.window, self.sinks, self.prompt_room = ctx, finished, window, sinks, prompt_room
+        self.prompt_ctx = B.Ctx(B_ * prompt_room, ctx.V, ctx.torch_dtype, stream=ctx.stream)
         self.layers = [(B.Layer(qkv), B.Layer(o)) for qkv, o in blocks]
         dim = blocks[0][1].shape[1] // heads
         self.split = [heads * dim, kv_heads * dim, kv_heads * dim]
@@ -70,12 +75,12 @@ class Attention:
             return
         qkv, o = (torch.empty(len(x), t.shape[1], dtype=x.dtype, device="cuda") for t in (self.qkv, self.o))
         for (to_qkv, to_x), cache in zip(self.layers, self.caches):
-            B.as_linear(self.ctx, to_qkv, x, qkv)
+            B.as_linear(self.prompt_ctx, to_qkv, x, qkv)
             q, k, v = qkv.split(self.split, dim=1)
-            B.as_cache_add(self.ctx, cache, self.prompts, k, v, offsets)
-            B.as_attend_prompts(self.ctx, cache, self.prompts, q, offsets, o, window=self.window, sinks=self.sinks)
+            B.as_cache_add(self.prompt_ctx, cache, self.prompts, k, v, offsets)
+            B.as_attend_prompts(self.prompt_ctx, cache, self.prompts, q, offsets, o, window=self.window, sinks=self.sinks)
             out = torch.empty_like(x)
-            B.as_linear(self.ctx, to_x, o, out, residual=x)
+            B.as_linear(self.prompt_ctx, to_x, o, out, residual=x)
             x = out
 
     def step(self, x):
@@ -92,15 +97,15 @@ class Attention:
 
 
 class ShapedDecoder:
-    """Decodes B prompts by N codes each, one token a step.  attention: Attention's blocks, heads, kv_heads, prompt_room (of all
-    prompts together, too), room and more, as a dict; none: the model goes by the last token."""
+    """Decodes B prompts by N codes each, one token a step.  attention: Attention's blocks, heads, kv_heads, prompt_room (the longest
+    prompt, without its last token), room (steps) and more, as a dict; none: the model goes by the last token."""
 
     def __init__(self, E, W1, b1, W2, b2, head, B_, N, grammar=None, bias=None, repetition=1.2, presence=0.2, frequency=0.1,
                  temp=0.8, top_k=0, top_p=0.95, eos_id=1, cap=30.0, stream=None, attention=None):
         V, d = E.shape
         self.E, self.V, self.N, self.rows = E, V, N, B_ * N
         self.temp, self.top_k, self.top_p, self.eos_id, self.grammar = temp, top_k, top_p, eos_id, grammar
-        self.ctx = B.Ctx(self.rows if attention is None else max(self.rows, B_ * attention["prompt_room"]), V, torch.bfloat16, stream=stream)
+        self.ctx = B.Ctx(self.rows, V, torch.bfloat16, stream=stream)
         self.up, self.down = B.Layer(W1, bias=b1, act="silu"), B.Layer(W2, bias=b2)
         self.head = B.Layer(head, act="softcap", act_arg=cap)
         new = lambda *shape, **kw: torch.zeros(*shape, device="cuda", **kw)  # noqa: E731
@@ -118,6 +123,10 @@ class ShapedDecoder:
 
     def start(self, prompts, u):
         """prompts: lists of token ids, one each; u: a shift of the lattice each."""
+        if len(prompts) * self.N != self.rows:
+            raise ValueError(f"{len(prompts)} prompts, not {self.rows // self.N}")
+        if self.attention is not None and max(map(len, prompts)) - 1 > self.attention.prompt_room:
+            raise ValueError(f"a prompt of more than {self.attention.prompt_room + 1} tokens")
         offsets = torch.tensor([0] + [len(p) for p in prompts]).cumsum(0).cuda()
         flat = torch.tensor([t for p in prompts for t in p], dtype=torch.int32, device="cuda")
         B.as_history_set(self.ctx, self.seen, self.counts, flat, offsets, self.N)
