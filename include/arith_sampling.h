@@ -683,7 +683,7 @@ as_status as_cache_add(as_ctx *ctx, const as_cache *cache, const as_sequences *s
  *              heads * head_dim apart; may start anywhere
  *              out must not overlap q, k or v
  *   heads      a multiple of kv_heads, at most AS_MAX_HEADS
- *   scale      finite (usually 1 / sqrt(head_dim))
+ *   scale      finite, and so scale * log2(e) (usually 1 / sqrt(head_dim))
  * The keys are split over the GPU where there are few rows, and those of prompts
  * taken for all their rows together: what the parts come to lies in a workspace of
  * the context, which is (re)allocated when a call needs more than any earlier one

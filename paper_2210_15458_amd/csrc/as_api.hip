@@ -1286,14 +1286,15 @@ static as_status check_queries(as_ctx *ctx, AttendArgs *a, const void *q, int64_
 {
     if (heads < 1 || heads > AS_MAX_HEADS || heads % a->kv_heads != 0)
         return fail(ctx, AS_ERR_INVALID_ARG, "heads must be a multiple of kv_heads in [1, AS_MAX_HEADS]");
-    if (!isfinite(scale)) return fail(ctx, AS_ERR_INVALID_ARG, "scale must be finite");
+    const float scale2 = scale * 1.44269504088896340736f;
+    if (!isfinite(scale2)) return fail(ctx, AS_ERR_INVALID_ARG, "scale must be finite, and its product with log2(e)");
     if (sinks < 0) return fail(ctx, AS_ERR_INVALID_ARG, "sinks is negative");
     if (a->tokens == 0) return AS_OK;
     if (!q || !out) return fail(ctx, AS_ERR_INVALID_ARG, "q and out must not be NULL");
     if (ldq < (int64_t)heads * a->dim || ldo < (int64_t)heads * a->dim) return fail(ctx, AS_ERR_INVALID_ARG, "ldq or ldo is smaller than its rows");
     if (!aligned_to(q, a->dtype) || !aligned_to(out, a->dtype)) return fail(ctx, AS_ERR_INVALID_ARG, "q or out is not aligned to its element type");
     a->q = q; a->ldq = ldq; a->out = out; a->ldo = ldo; a->heads = heads; a->group = heads / a->kv_heads;
-    a->scale = scale * 1.44269504088896340736f;
+    a->scale = scale2;
     // (as wide as the tables' rooms is none; one that is left fits 32 bits when it is taken off any position)
     a->window = window > 0 && window < (int64_t)a->prompt_room + a->room ? window : 0;
     a->sinks = sinks;
