@@ -590,7 +590,9 @@ def _heads_of(cache, q):
     return heads, cols
 
 
-_MOST = 0x7fffffff
+def _int32(x):
+    """The nearest to x that an int32 holds (which ctypes would take the lowest bits for)."""
+    return x if -0x80000000 <= x <= 0x7fffffff else 0x7fffffff if x > 0 else -0x80000000
 
 
 def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
@@ -601,7 +603,7 @@ def as_attend(ctx, cache, seqs, q, out, scale=None, window=0, sinks=0):
     qp, ldq = _tokens_of(cache, q, "q", rows, cols)
     op, ldo = _tokens_of(cache, out, "out", rows, cols)
     rc = (_lib or lib()).as_attend(ctx._h, cache._ref, seqs._ref, rows, qp, ldq, heads, cache.scale if scale is None else float(scale),
-                                   window if window < _MOST else _MOST, sinks if sinks < _MOST else _MOST, op, ldo)
+                                   _int32(window), _int32(sinks), op, ldo)
     if rc:
         ctx._check(rc)
 
@@ -614,6 +616,6 @@ def as_attend_prompts(ctx, cache, seqs, q, offsets, out, scale=None, window=0, s
     qp, ldq = _tokens_of(cache, q, "q", n, cols)
     op, ldo = _tokens_of(cache, out, "out", n, cols)
     rc = (_lib or lib()).as_attend_prompts(ctx._h, cache._ref, seqs._ref, seqs.rows, qp, ldq, n, at, heads, cache.scale if scale is None else float(scale),
-                                           window if window < _MOST else _MOST, sinks if sinks < _MOST else _MOST, op, ldo)
+                                           _int32(window), _int32(sinks), op, ldo)
     if rc:
         ctx._check(rc)
