@@ -295,8 +295,8 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs &a, const Work &
 // 16 a + 4 q + j (a: 16 tokens of the tile, j < 4), and hands them to the second as its share of the sum over tokens, which may go
 // in any order as long as V^T's lanes have the same tokens: so V is read in whole rows, 16 lanes one token, and the 2-byte
 // values of a lane's tokens are put in pairs by byte permutations, without LDS.
-// Bound by the memory where rows are long (8 rows of up to 65536 tokens, 8 key heads of 128, bf16: 294 us, 5.3 TB/s; 256 rows that see 1028
-// each 100 us, 5.8), by one tile after the other where they are short (about 1.1 us each).  A tile's keys are asked for as soon as
+// Bound by the memory where rows are long (8 rows of up to 65536 tokens, 8 key heads of 128, bf16: 295 us, 5.3 TB/s, and 7 us of joining;
+// 256 rows that see 1028 each 101 us, 5.7), by one tile after the other where they are short (about 1.1 us each).  A tile's keys are asked for as soon as
 // the scores of the one before it are taken, its values behind that one's product, into the same registers (305 -> 301, fp32 prompts 35 -> 32).
 template <class T, int DP> struct AttendForm;
 template <int DP> struct AttendForm<uint16_t, DP> {
@@ -656,10 +656,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, const AttendPie
 // In LDS a row's 16-byte pieces are exchanged (by its number, piece c at c ^ f(row)), so that neither the rows that 16 lanes
 // read of K nor the four rows they read of V meet in a bank.
 // A query's reference m is raised only when a score passes it by 2^8: weights up to 256 are as good as weights up to 1.
-// Bound by the matrix pipes and the clock that their power leaves: 8192 tokens, 32 heads of 128 over 8, causal, 512 us = 1.07 PFLOP/s,
-// pipes busy 52 % of the cycles at 2.0 GHz (a library product of 8192^3 has 1.37).  On the way: 625 us with the compiler's own
-// requests, which it waited for before each read of LDS; 575 by hand; 542 with the next tile's products under this tile's
-// exponentials; 512 with the waves' products put before other waves' work and fewer scalar instructions a tile.
+// Bound by the matrix pipes and the clock that their power leaves: 8192 tokens, 32 heads of 128 over 8, causal, 510 to 527 us from card to
+// card = 1.04 to 1.08 PFLOP/s, pipes busy 54 % of the cycles (a library product of 8192^3 has 1.37).  On the way: 625 us with the
+// compiler's own requests, which it waited for before each read of LDS; 575 by hand; 542 with the next tile's products under this
+// tile's exponentials; 522 with the waves' products put before other waves' work and fewer scalar instructions a tile; 515 with
+// maxima of products in place of scores.
 template <int DP> struct TileForm {
     static constexpr int kKeys = DP == 256 ? 32 : 64, kPieces = DP / 8, kBytes = kKeys * DP * 2, kLoads = kBytes / 4096, kRowsEach = 64 / kPieces;
     static constexpr int kQueries = 128, kStride = 68;
